@@ -370,6 +370,154 @@ cqsa_status cqsa_forward_noalloc(const cqsa_plan_t* plan, const cqsa_tensor* Q,
                                  const cqsa_tensor* K, const cqsa_tensor* V, cqsa_tensor* O,
                                  float* LSE, cqsa_mem lse_where, float scale, void* hip_stream);
 
+/* ------------------------------------------------------------------------
+ * Operators around attention: rotary positions on Q and K, and a paged
+ * key-value cache in 4 bits with the attention that reads it.
+ *
+ * Their tensors are views of device memory with strides, so that Q, K and V
+ * may be parts of one fused projection.  Every call is enqueued on
+ * `hip_stream` and returns without waiting; it allocates nothing, keeps no
+ * state between calls and may be captured into a graph.  A check that fails
+ * reports CQSA_ERR_INVALID_ARG before any device work.  What a call reads from
+ * device memory (positions, page tables, lengths) is not checked on the host:
+ * the kernels clamp it, so that no value makes them leave the buffers.  All
+ * tensors of a call live on the device that is current at the call.
+ * ---------------------------------------------------------------------- */
+
+/* A [B, L, H, d] tensor in device memory.  Strides are in elements, 0 or more,
+ * and that of d is 1; `data` and, along axes of two or more elements, the
+ * strides are multiples of 16 bytes.  Elements that a call writes must not
+ * overlap.  An empty tensor (B, L or H = 0) may have data = NULL. */
+typedef struct {
+  void* data;
+  cqsa_dtype dtype;
+  int64_t B, L, H, d;
+  int64_t stride_b, stride_l, stride_h;
+} cqsa_view;
+
+#define CQSA_MAX_AXES 4
+#define CQSA_PAIR_HALF 0       /* pair i of n: elements i and i + n */
+#define CQSA_PAIR_ADJACENT 1   /* pair i: elements 2 i and 2 i + 1 */
+#define CQSA_SPECTRUM_SHARED 0 /* pair i of n turns theta^(-i / n) radians a position */
+#define CQSA_SPECTRUM_AXIS 1   /* pair j of the m of its axis: theta^(-j / m) */
+
+/* Rotary positions with n_axes coordinates a token (text: 1; images: height and
+ * width; video: time, height, width).  sections[a] pairs turn with axis a's
+ * coordinate; n = sum of sections, and elements 2 n .. d - 1 stay as they are. */
+typedef struct {
+  int32_t d;                       /* head dimension: a multiple of 32 in [32, 256] */
+  int32_t n_axes;                  /* 1 .. CQSA_MAX_AXES (1) */
+  int32_t sections[CQSA_MAX_AXES]; /* >= 1 each, n a multiple of 8, 2 n <= d ({d / 2}) */
+  int32_t pairs;                   /* CQSA_PAIR_* (half) */
+  int32_t spectrum;                /* CQSA_SPECTRUM_* (shared) */
+  int32_t dealt;                   /* 0: the axes' pairs follow one another; 1: they are dealt to
+                                      the axes in turn, an axis whose section is full left out (0) */
+  double theta;                    /* > 1 (10000) */
+  double pos_scale[CQSA_MAX_AXES]; /* coordinates are multiplied by this, > 0 and finite (1) */
+} cqsa_rotary_opts;
+
+typedef struct cqsa_rotary_s cqsa_rotary_t;
+
+/* Fill `o` with the defaults noted in cqsa_rotary_opts for head dimension d. */
+void cqsa_rotary_opts_default(cqsa_rotary_opts* o, int32_t d);
+/* The rotation's table, made once for all calls.  Host only.  *out receives a
+ * plan that the caller must destroy; it is immutable and may be shared. */
+cqsa_status cqsa_rotary_plan(const cqsa_rotary_opts* opts, cqsa_rotary_t** out);
+void cqsa_rotary_destroy(cqsa_rotary_t* plan); /* NULL is a no-op */
+
+/* y[k] = x[k] with every pair (a, b) of every token's every head turned by the
+ * pair's angle w = pos_scale * pos * (its turn a position):
+ * (a cos w - b sin w, b cos w + a sin w).  inverse = 1 turns by -w: the
+ * gradient of x[k] from that of y[k].  n = 1 or 2 tensors (Q, or Q and K) are
+ * turned in one launch; they share B, L, d and the dtype.  y[k] may be x[k]
+ * itself (same data and strides).  pos: int32 [n_axes, B, L] in device memory,
+ * any value: angles are reduced in 64-bit fixed point (2^-64 turns a position,
+ * so 2^-33 turns at the farthest), and the products are fp32, rounded once. */
+cqsa_status cqsa_rotary(const cqsa_rotary_t* plan, const int32_t* pos, const cqsa_view* x,
+                        const cqsa_view* y, int32_t n, int32_t inverse, void* hip_stream);
+
+/* A paged cache of keys and values in 4 bits.  Elements are e2m1 (0, .5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives); 32 elements along d share a power of
+ * two, stored in a byte as its exponent plus 127.  A block's power is
+ * 2^(e - 2), e the exponent of its largest magnitude a, or one more where
+ * a >= 1.75 * 2^e (which would round past 6), from 2^-127 to 2^125; elements
+ * are rounded to nearest even and end at 6.  A block with an infinity or a NaN gets the byte 255 and
+ * stands for NaN throughout.  bf16 and fp32 hold every value of the cache
+ * exactly.  17 bytes for 32 elements: 3.76 times less than bf16.
+ *
+ * Layout: page p of `page_size` tokens starts at data + p * page_bytes and holds
+ * [H][page_size / 32] tiles of 34 d bytes, one head's 32 tokens each:
+ *   K codes      [d / 32][32 tokens][16]
+ *   V codes      [d / 32][16 pairs][4][2][4], token 16 b + 4 a + c at [a][b][c]
+ *   K exponents  [16][d / 32][2], token 16 b + a at [a][.][b]
+ *   V exponents  [4][d / 32][2][4], tokens as in V's codes
+ * where a byte of codes is elements 2 i (low half) and 2 i + 1 of its token.
+ * K's order is the operand of the matrix instruction that takes such codes as
+ * they are; V's lets a lane load the tokens that its operand holds together. */
+typedef struct {
+  void* data;        /* device memory, 64-byte aligned, n_pages * page_bytes */
+  int64_t n_pages;
+  int32_t page_size; /* 32, 64, 128 or 256 tokens */
+  int32_t H;         /* heads of keys and values */
+  int32_t d;         /* a multiple of 32 in [32, 256] */
+} cqsa_cache;
+
+/* Bytes of one page of such a cache (host only); 0 if an argument is not allowed. */
+uint64_t cqsa_cache_page_bytes(int32_t page_size, int32_t H, int32_t d);
+
+/* The sequences of a call.  Sequence b's token t is in page
+ * pages[b * pages_stride + t / page_size].  lengths[b] is the number of its
+ * tokens in the cache once the call's are written; the call's n_b tokens are
+ * the last ones, at positions lengths[b] - n_b ... lengths[b] - 1.
+ * q_start = NULL: n_b = L, and the tensors are [B, L, ., d].  Else the tensors
+ * are packed, [1, T, ., d] (LSE [1, H, T]), sequence b has rows q_start[b] ...
+ * q_start[b + 1] - 1, and rows that no sequence has are neither read nor
+ * written.  A page entry outside [0, n_pages) holds nothing: writing to it is
+ * dropped, reading from it gives zeros and attention leaves its tokens out, so
+ * such entries may stand for tokens that a caller has given up.
+ * Values outside their range are taken as the nearest one allowed: lengths in
+ * [0, max_len], q_start in [0, T] and not falling, n_b at most max_q. */
+typedef struct {
+  const int32_t* pages;   /* device [B, max_pages] */
+  int64_t pages_stride;   /* elements between two sequences' tables, >= max_pages */
+  const int32_t* lengths; /* device [B] */
+  const int32_t* q_start; /* device [B + 1], or NULL */
+  int32_t B;
+  int32_t max_pages;
+  int32_t max_len; /* host's bound on the lengths, <= max_pages * page_size; it sizes the launch */
+  int32_t max_q;   /* host's bound on n_b with q_start, >= 1 and at most T; ignored without */
+} cqsa_cache_batch;
+
+/* Quantise the call's K and V rows (same shape and dtype, any of the three) into the
+ * cache.  A row before position 0 (n_b > lengths[b]) is dropped.  Two rows must not have
+ * the same page and place. */
+cqsa_status cqsa_cache_write(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                             const cqsa_view* K, const cqsa_view* V, void* hip_stream);
+/* The values that the cache holds for the call's rows, into K and V (same shape and dtype):
+ * what cqsa_cache_write wrote, or with n_b = lengths[b] whole sequences for cqsa_forward.
+ * Exact in bf16 and fp32, rounded to nearest even in fp16.  Rows before position 0 are zero. */
+cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                            const cqsa_view* K, const cqsa_view* V, void* hip_stream);
+
+/* Attention of the call's rows Q (H_q heads, a multiple of the cache's H; head h reads the
+ * cache's head h / (H_q / H)) over their sequences' cached tokens: with causal = 1 row i of
+ * sequence b sees positions 0 ... lengths[b] - n_b + i, with 0 all of them.  O: Q's shape
+ * and dtype; LSE (or NULL): fp32 [B, H_q, L], the natural logarithm of the sum of the
+ * exponentials of the scaled scores.  A row that sees nothing gets O = 0 and LSE =
+ * -infinity.  A NaN in a token reaches only rows that see it.  scale <= 0 selects
+ * 1 / sqrt(d).  Scores and the softmax are fp32 for every dtype.
+ * workspace: device memory of at least cqsa_cache_attend_workspace bytes, 16-byte aligned,
+ * with any contents; NULL where that is 0.  Calls that may overlap, replays of captured
+ * graphs among them, need workspaces of their own. */
+cqsa_status cqsa_cache_attend(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                              const cqsa_view* Q, const cqsa_view* O, float* LSE, int32_t causal,
+                              float scale, void* workspace, uint64_t workspace_bytes,
+                              void* hip_stream);
+/* Host only: the workspace of such a call, by the sizes of its arguments alone (Q's data
+ * is not read).  *bytes may be 0. */
+cqsa_status cqsa_cache_attend_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                                        const cqsa_view* Q, uint64_t* bytes);
+
 /* Route the library's device workspace through a caller allocator (e.g. a
  * framework's caching allocator).  alloc(bytes, ctx) returns device memory or
  * NULL (reported as CQSA_ERR_DEVICE_OOM); release(ptr, ctx) frees it.  Passing

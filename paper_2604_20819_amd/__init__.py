@@ -80,6 +80,33 @@ class cqsa_run_stats(ctypes.Structure):
                 ("kernel_kv_tiles_mixed", ctypes.c_int64)]
 
 
+class cqsa_view(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("B", ctypes.c_int64),
+                ("L", ctypes.c_int64), ("H", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("stride_b", ctypes.c_int64), ("stride_l", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64)]
+
+
+class cqsa_rotary_opts(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4),
+                ("pairs", ctypes.c_int32), ("spectrum", ctypes.c_int32), ("dealt", ctypes.c_int32),
+                ("theta", ctypes.c_double), ("pos_scale", ctypes.c_double * 4)]
+
+
+class cqsa_cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("H", ctypes.c_int32), ("d", ctypes.c_int32)]
+
+
+class cqsa_cache_batch(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("pages_stride", ctypes.c_int64),
+                ("lengths", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+                ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("max_q", ctypes.c_int32)]
+
+
+_V, _C, _CB = (ctypes.POINTER(x) for x in (cqsa_view, cqsa_cache, cqsa_cache_batch))
+
 # Every symbol include/cqsa.h declares, with its ctypes signature.
 _SIGS = {
     "cqsa_plan_opts_default": (None, [ctypes.POINTER(cqsa_plan_opts)]),
@@ -118,6 +145,19 @@ _SIGS = {
                                      ctypes.POINTER(cqsa_tensor), ctypes.POINTER(cqsa_tensor),
                                      ctypes.POINTER(cqsa_tensor), ctypes.POINTER(cqsa_tensor),
                                      ctypes.c_float, ctypes.c_void_p]),
+    "cqsa_rotary_opts_default": (None, [ctypes.POINTER(cqsa_rotary_opts), ctypes.c_int32]),
+    "cqsa_rotary_plan": (ctypes.c_int, [ctypes.POINTER(cqsa_rotary_opts),
+                                        ctypes.POINTER(ctypes.c_void_p)]),
+    "cqsa_rotary_destroy": (None, [ctypes.c_void_p]),
+    "cqsa_rotary": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, _V, _V, ctypes.c_int32,
+                                   ctypes.c_int32, ctypes.c_void_p]),
+    "cqsa_cache_page_bytes": (ctypes.c_uint64, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "cqsa_cache_write": (ctypes.c_int, [_C, _CB, _V, _V, ctypes.c_void_p]),
+    "cqsa_cache_read": (ctypes.c_int, [_C, _CB, _V, _V, ctypes.c_void_p]),
+    "cqsa_cache_attend": (ctypes.c_int, [_C, _CB, _V, _V, ctypes.c_void_p, ctypes.c_int32,
+                                         ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64,
+                                         ctypes.c_void_p]),
+    "cqsa_cache_attend_workspace": (ctypes.c_int, [_C, _CB, _V, ctypes.POINTER(ctypes.c_uint64)]),
     "cqsa_set_allocator": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "cqsa_set_timing": (ctypes.c_int, [ctypes.c_int32]),
     "cqsa_set_tile_counting": (ctypes.c_int, [ctypes.c_int32]),
@@ -362,6 +402,210 @@ def cqsa_backward(plan, Q, K, V, O, LSE, dO, dQ, dK, dV, scale=0.0, stream=None)
                                CQSA_MEM_DEVICE if LSE.is_cuda else CQSA_MEM_HOST,
                                *(ctypes.byref(t) for t in ts[4:]), float(scale), s),
            "cqsa_backward")
+
+
+# ------------------------------------------- rotary positions, 4-bit cache
+def as_cqsa_view(t):
+    """Describe a [B, L, H, d] torch tensor on a GPU, strided or not (no copy)."""
+    if t.dim() != 4:
+        raise ValueError("tensors must be [B, L, H, d]")
+    if not t.is_cuda:
+        raise ValueError("tensors must live on a GPU")
+    (B, L, H, d), (sb, sl, sh, sd) = t.shape, t.stride()
+    if sd != 1:
+        raise ValueError("the last dimension must be contiguous")
+    return cqsa_view(t.data_ptr(), _dtype_code(t), B, L, H, d, sb, sl, sh)
+
+
+def _device_array(t, name, shape):
+    """An int32 array that the C ABI takes as a bare pointer."""
+    if t.dtype != _torch().int32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor on a GPU")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+
+
+def _one_device(*ts):
+    d = ts[0].device
+    for t in ts:
+        if t is not None and t.device != d:
+            raise ValueError("all tensors of a call must live on one device")
+    return d
+
+
+def _enqueue(what, device, stream, call):
+    """call(stream) with `device` current, on `stream` or the device's current one."""
+    torch = _torch()
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _enqueue(what, device, stream, call)
+    if stream is None:
+        stream = torch.cuda.current_stream(device).cuda_stream
+    _check(call(stream), what)
+
+
+class RotaryPlan:
+    """Owner of a cqsa_rotary_t*."""
+
+    def __init__(self, handle, opts):
+        self.handle, self.opts = handle, opts
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.cqsa_rotary_destroy(self.handle)
+            self.handle = None
+
+
+def cqsa_rotary_plan(d, sections=None, theta=10000.0, pairs="half", spectrum="shared", dealt=False,
+                     pos_scale=None):
+    """The table of a rotation (host only).  sections: pairs of each axis (None:
+    one axis, all d / 2); pairs: "half" or "adjacent"; spectrum: "shared" or
+    "per_axis"; dealt: pairs dealt to the axes in turn; pos_scale: a factor of
+    each axis's positions."""
+    o = cqsa_rotary_opts()
+    lib().cqsa_rotary_opts_default(ctypes.byref(o), d)
+    o.pairs = {"half": 0, "adjacent": 1}[pairs]
+    o.spectrum = {"shared": 0, "per_axis": 1}[spectrum]
+    o.dealt, o.theta = int(bool(dealt)), theta
+    if sections is not None:
+        if len(sections) > 4:
+            raise ValueError("at most 4 axes")
+        o.n_axes = len(sections)
+        for a, n in enumerate(sections):
+            o.sections[a] = n
+    if pos_scale is not None:
+        if len(pos_scale) != o.n_axes:
+            raise ValueError("pos_scale needs a factor for each axis")
+        for a, f in enumerate(pos_scale):
+            o.pos_scale[a] = f
+    h = ctypes.c_void_p()
+    _check(lib().cqsa_rotary_plan(ctypes.byref(o), ctypes.byref(h)), "cqsa_rotary_plan")
+    return RotaryPlan(h.value, o)
+
+
+def cqsa_rotary(plan, pos, x, y=None, inverse=False, stream=None):
+    """Turn x (a [B, L, H, d] tensor, or a list of one or two: Q, or Q and K)
+    into y (None: in place) by positions pos, int32 [axes, B, L].  inverse=True
+    gives the gradient of x from that of y."""
+    xs = [x] if hasattr(x, "data_ptr") else list(x)
+    ys = xs if y is None else [y] if hasattr(y, "data_ptr") else list(y)
+    n = len(xs)
+    if n not in (1, 2) or len(ys) != n:
+        raise ValueError("one or two tensors, and as many results")
+    _device_array(pos, "pos", (plan.opts.n_axes, xs[0].shape[0], xs[0].shape[1]))
+    device = _one_device(pos, *xs, *ys)
+    vx = (cqsa_view * n)(*map(as_cqsa_view, xs))
+    vy = vx if ys is xs else (cqsa_view * n)(*map(as_cqsa_view, ys))
+    _enqueue("cqsa_rotary", device, stream,
+             lambda s: lib().cqsa_rotary(plan.handle, pos.data_ptr(), vx, vy, n, int(bool(inverse)), s))
+
+
+def cqsa_cache_page_bytes(page_size, H, d):
+    """Bytes of one page of the 4-bit cache (cqsa_cache_page_bytes)."""
+    return lib().cqsa_cache_page_bytes(page_size, H, d)
+
+
+class Cache4:
+    """A paged 4-bit cache of keys and values (cqsa_cache): n_pages pages of
+    page_size tokens of H heads.  data: a contiguous uint8 tensor to keep it in
+    (None: a new one of zeros on `device`)."""
+
+    def __init__(self, n_pages, H, d, page_size=64, data=None, device="cuda"):
+        torch = _torch()
+        per = cqsa_cache_page_bytes(page_size, H, d)
+        if per == 0:
+            raise ValueError("page_size must be 32, 64, 128 or 256, H in [1, 65536], "
+                             "d a multiple of 32 in [32, 256]")
+        if data is None:
+            data = torch.zeros((n_pages, per), dtype=torch.uint8, device=device)
+        if data.dtype != torch.uint8 or not data.is_cuda or not data.is_contiguous():
+            raise ValueError("data must be a contiguous uint8 tensor on a GPU")
+        if data.numel() != n_pages * per:
+            raise ValueError(f"data must have {n_pages} x {per} bytes")
+        self.n_pages, self.H, self.d, self.page_size = n_pages, H, d, page_size
+        self.data = data
+        self.view = cqsa_cache(data.data_ptr(), n_pages, page_size, H, d)
+
+
+class CacheBatch:
+    """The sequences of a call (cqsa_cache_batch).  pages: int32 [B, max_pages];
+    lengths: int32 [B], the tokens in the cache with the call's; q_start: int32
+    [B + 1] for packed rows, then max_q bounds a sequence's rows.  max_len bounds
+    the lengths (0: the table's tokens, once a cache says how many)."""
+
+    def __init__(self, pages, lengths, q_start=None, max_len=0, max_q=0):
+        if pages.dim() != 2 or pages.dtype != _torch().int32 or not pages.is_cuda or \
+                (pages.shape[1] > 1 and pages.stride(1) != 1):
+            raise ValueError("pages must be an int32 tensor [B, max_pages] on a GPU with contiguous rows")
+        B, n = pages.shape
+        _device_array(lengths, "lengths", (B,))
+        if q_start is not None:
+            _device_array(q_start, "q_start", (B + 1,))
+        self.pages, self.lengths, self.q_start = pages, lengths, q_start
+        self.max_len, self.max_q, self.device = max_len, max_q, _one_device(pages, lengths, q_start)
+        self.view = cqsa_cache_batch(pages.data_ptr(), pages.stride(0) if B > 1 else n, lengths.data_ptr(),
+                                     q_start.data_ptr() if q_start is not None else None, B, n,
+                                     max_len, max_q)
+
+    def _of(self, cache, t):
+        """The descriptor for a cache and a tensor of rows: the bounds left open filled in."""
+        if self.max_len and (self.max_q or self.q_start is None):
+            return self.view
+        v = cqsa_cache_batch.from_buffer_copy(self.view)
+        if not self.max_len:
+            v.max_len = min(v.max_pages * cache.page_size, 2 ** 31 - 1)
+        if not self.max_q:
+            v.max_q = t.shape[1]
+        return v
+
+
+def _cache_move(what, cache, batch, K, V, stream):
+    device = _one_device(cache.data, batch.pages, K, V)
+    vk, vv, vb = as_cqsa_view(K), as_cqsa_view(V), batch._of(cache, K)
+    _enqueue(what, device, stream, lambda s: getattr(lib(), what)(cache.view, vb, vk, vv, s))
+
+
+def cqsa_cache_write(cache, batch, K, V, stream=None):
+    """Quantise the call's rows of K and V into the cache's pages."""
+    _cache_move("cqsa_cache_write", cache, batch, K, V, stream)
+
+
+def cqsa_cache_read(cache, batch, K, V, stream=None):
+    """Fill K and V with the values that the cache holds for the call's rows."""
+    _cache_move("cqsa_cache_read", cache, batch, K, V, stream)
+
+
+def cqsa_cache_attend_workspace(cache, batch, Q):
+    """A workspace for cqsa_cache_attend with arguments of these sizes (a uint8
+    tensor, or None where none is needed); calls that may overlap need their own."""
+    n = ctypes.c_uint64()
+    _check(lib().cqsa_cache_attend_workspace(cache.view, batch._of(cache, Q), as_cqsa_view(Q), n),
+           "cqsa_cache_attend_workspace")
+    return _torch().empty(n.value, dtype=_torch().uint8, device=Q.device) if n.value else None
+
+
+def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, workspace=None, stream=None):
+    """Attention of the call's rows Q over their sequences' cached tokens into O
+    and, if given, LSE (fp32 [B, Hq, L], packed [1, Hq, T]).  workspace=None
+    takes one from torch for this call."""
+    torch = _torch()
+    if LSE is not None:
+        want = (Q.shape[0], Q.shape[2], Q.shape[1])
+        if LSE.dtype != torch.float32 or not LSE.is_contiguous() or tuple(LSE.shape) != want:
+            raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {want}")
+    device = _one_device(cache.data, batch.pages, Q, O, LSE, workspace)
+    if workspace is None:
+        workspace = cqsa_cache_attend_workspace(cache, batch, Q)
+        if workspace is not None and stream is not None:
+            workspace.record_stream(torch.cuda.ExternalStream(stream, device=device))
+    elif not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    vq, vo, vb = as_cqsa_view(Q), as_cqsa_view(O), batch._of(cache, Q)
+    _enqueue("cqsa_cache_attend", device, stream,
+             lambda s: lib().cqsa_cache_attend(
+                 cache.view, vb, vq, vo, LSE.data_ptr() if LSE is not None else None,
+                 int(bool(causal)), float(scale), workspace.data_ptr() if workspace is not None else None,
+                 workspace.numel() * workspace.element_size() if workspace is not None else 0, s))
 
 
 def cqsa_set_timing(enable):

@@ -25,7 +25,9 @@ COMMON = [
 ]
 SOURCES = [
     "plan.cpp", "capi_plan.cpp", "runtime.cpp", "fwd_driver.cpp", "bwd_driver.cpp", "guard.cpp",
+    "rotary_driver.cpp", "cache_driver.cpp",
     "attn_fwd.hip", "merge.hip", "attn_bwd.hip", "stage.hip",
+    "rotary.hip", "cache_quant.hip", "cache_attend.hip",
 ]
 
 
