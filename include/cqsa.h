@@ -452,8 +452,8 @@ cqsa_status cqsa_rotary(const cqsa_rotary_t* plan, const int32_t* pos, const cqs
  *   K exponents  [16][d / 32][2], token 16 b + a at [a][.][b]
  *   V exponents  [4][d / 32][2][4], tokens as in V's codes
  * where a byte of codes is elements 2 i (low half) and 2 i + 1 of its token.
- * K's order is the operand of the matrix instruction that takes such codes as
- * they are; V's lets a lane load the tokens that its operand holds together. */
+ * K's order gives a lane 32 elements of a token in 16 bytes; V's, the tokens
+ * that an operand of the weights' product holds together. */
 typedef struct {
   void* data;        /* device memory, 64-byte aligned, n_pages * page_bytes */
   int64_t n_pages;

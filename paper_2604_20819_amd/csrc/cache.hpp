@@ -49,11 +49,24 @@ struct AttendArgs {
   int32_t Hq, G;     // query heads, and of them for each head of the cache
   int32_t causal;
   float scale_log2;  // softmax scale * log2(e)
+  // with splits: every row's (by its place in LSE) and split's unnormalised
+  // result, its shift (log2) and sum
+  float* part;
+  float* part_ml;
 };
+
+// How a call's rows and tokens are spread over work groups; by its sizes alone.
+struct AttendPlan {
+  int row_groups;  // of 16 rows, for each wave
+  int row_tiles;   // work groups over a sequence's and head's rows
+  int splits;      // work groups over a sequence's tokens
+};
+// rows: the most that a sequence and key head has.
+AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
 
 hipError_t launch_cache_write(cqsa_dtype dt, const CacheMoveArgs& a, hipStream_t s);
 hipError_t launch_cache_read(cqsa_dtype dt, const CacheMoveArgs& a, hipStream_t s);
-hipError_t launch_cache_attend(cqsa_dtype dt, const AttendArgs& a, hipStream_t s);
+hipError_t launch_cache_attend(cqsa_dtype dt, const AttendArgs& a, const AttendPlan& p, hipStream_t s);
 
 #ifdef __HIPCC__
 

@@ -112,6 +112,16 @@ cqsa_status move_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa
   return CQSA_OK;
 }
 
+// The launch of a call whose arguments check_attend has passed, and its workspace.
+AttendPlan attend_plan(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view& Q) {
+  const int64_t n = b->q_start ? b->max_q : Q.L;
+  return plan_attend(b->B, c->H, n * (Q.H / c->H), b->max_len, Q.dtype, c->d);
+}
+uint64_t attend_bytes(const AttendPlan& p, const cqsa_view& Q) {
+  if (p.splits == 1) return 0;
+  return uint64_t(Q.B) * uint64_t(Q.L) * uint64_t(Q.H) * uint64_t(p.splits) * uint64_t(Q.d + 4) * 4;
+}
+
 cqsa_status check_attend(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view* Q,
                          const std::string& what) {
   cqsa_status st;
@@ -120,7 +130,12 @@ cqsa_status check_attend(const cqsa_cache* c, const cqsa_cache_batch* b, const c
   if (!Q) return fail(CQSA_ERR_INVALID_ARG, what + "Q is NULL");
   if (Q->H < c->H || Q->H % c->H != 0 || Q->H > kMaxHeads)
     return fail(CQSA_ERR_INVALID_ARG, what + "Q's heads must be a multiple of the cache's, at most 65536");
-  return check_rows(b, *Q, what);
+  if ((st = check_view(Q, "Q", c->d, false)) != CQSA_OK) return st;
+  if ((st = check_rows(b, *Q, what)) != CQSA_OK) return st;
+  const int64_t n = b->q_start ? b->max_q : Q->L;
+  if (n * (Q->H / c->H) > (int64_t(1) << 30) || n * (Q->H / c->H) * c->H * b->B > (int64_t(1) << 30))
+    return fail(CQSA_ERR_UNSUPPORTED, what + "more rows than one launch takes");
+  return CQSA_OK;
 }
 
 cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view* Q,
@@ -129,7 +144,6 @@ cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   const std::string what = "cqsa_cache_attend: ";
   cqsa_status st;
   if ((st = check_attend(c, b, Q, what)) != CQSA_OK) return st;
-  if ((st = check_view(Q, "Q", c->d, false)) != CQSA_OK) return st;
   if ((st = check_view(O, "O", c->d, true)) != CQSA_OK) return st;
   if (!same_shape(*Q, *O)) return fail(CQSA_ERR_INVALID_ARG, what + "O differs from Q in shape or dtype");
   if (causal != 0 && causal != 1) return fail(CQSA_ERR_INVALID_ARG, what + "causal must be 0 or 1");
@@ -147,9 +161,19 @@ cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   a.G = int32_t(Q->H / c->H);
   a.causal = causal;
   a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(float(c->d))) * 1.4426950408889634f;
-  (void)workspace;
-  (void)workspace_bytes;
-  CQSA_HIP(launch_cache_attend(Q->dtype, a, s));
+  const AttendPlan p = attend_plan(c, b, *Q);
+  const uint64_t need = attend_bytes(p, *Q);
+  if (need > 0) {
+    if (!workspace || workspace_bytes < need)
+      return fail(CQSA_ERR_INVALID_ARG, what + "the workspace has " + std::to_string(workspace ? workspace_bytes : 0) +
+                                            " bytes, the call needs " + std::to_string(need));
+    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
+      return fail(CQSA_ERR_INVALID_ARG, what + "the workspace must be 16-byte aligned");
+    const int64_t parts = Q->B * Q->L * Q->H * p.splits;
+    a.part = (float*)workspace;
+    a.part_ml = a.part + parts * c->d;
+  }
+  CQSA_HIP(launch_cache_attend(Q->dtype, a, p, s));
   return CQSA_OK;
 }
 
@@ -200,7 +224,10 @@ static cqsa_status workspace_impl(const cqsa_cache* cache, const cqsa_cache_batc
   const std::string what = "cqsa_cache_attend_workspace: ";
   if (!bytes) return fail(CQSA_ERR_INVALID_ARG, what + "bytes is NULL");
   *bytes = 0;
-  return check_attend(cache, batch, Q, what);
+  const cqsa_status st = check_attend(cache, batch, Q, what);
+  if (st != CQSA_OK || empty(*Q) || batch->B == 0) return st;
+  *bytes = attend_bytes(attend_plan(cache, batch, *Q), *Q);
+  return CQSA_OK;
 }
 
 cqsa_status cqsa_cache_attend_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,

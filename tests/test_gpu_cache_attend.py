@@ -1,11 +1,9 @@
 """Attention over the 4-bit cache on the GPU, against oracle.cache4 in float64.
 
 Bounds, from the arithmetic.  With t = the largest sum of |q k| scale of a key
-that the row sees: a score is off by at most e = t (2^-20 + d 2^-23): the
-queries' split into matrix operands leaves out under 2^-21 of each block's
-largest magnitude (taken against the keys' largest, 2^-20 covers what a block
-holds unevenly where its sum is within a factor of the product of maxima; the
-inputs here are normal, with d products a sum), and d products add up in fp32
+that the row sees: a score is off by at most e = t (2^-20 + d 2^-23): the scale,
+its products and the change to powers of two round by under 2^-20 of it, the
+products of its d terms are exact or rounded by half a step, and add up in fp32
 with an error of at most half a step each.  LSE is then off by e, and by 2^-22
 (|LSE| + 8) for the logarithm, the sum and the shift.  The weights are off by
 2 e and their rounding u relative to themselves (u = 2^-8 for bf16, whose
