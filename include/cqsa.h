@@ -484,7 +484,7 @@ typedef struct {
   const int32_t* q_start; /* device [B + 1], or NULL */
   int32_t B;
   int32_t max_pages;
-  int32_t max_len; /* host's bound on the lengths, <= max_pages * page_size; it sizes the launch */
+  int32_t max_len; /* host's bound on the lengths, <= max_pages * page_size and 2^30; it sizes the launch */
   int32_t max_q;   /* host's bound on n_b with q_start, >= 1 and at most T; ignored without */
 } cqsa_cache_batch;
 

@@ -11,6 +11,7 @@ Names follow include/cqsa.h: ``cqsa_plan``, ``cqsa_forward``,
 """
 import ctypes
 import os
+import struct
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libcqsa.so")
@@ -417,31 +418,77 @@ def as_cqsa_view(t):
     return cqsa_view(t.data_ptr(), _dtype_code(t), B, L, H, d, sb, sl, sh)
 
 
+# The calls of the operators: a step of decoding makes several of a few
+# microseconds each, so views are packed straight into cqsa_view's bytes (a
+# third of a ctypes structure's time).
+_VIEW = struct.Struct("=Qi4x7q")
+_calls = {}
+
+
+def _call(name):
+    """The library's function, with the cqsa_view arguments as bytes."""
+    f = _calls.get(name)
+    if f is None:
+        res, args = _SIGS[name]
+        lib()
+        f = ctypes.CDLL(LIB_PATH)[name]
+        f.restype, f.argtypes = res, [ctypes.c_char_p if x is _V else x for x in args]
+        _calls[name] = f
+    return f
+
+
+def _view(t, device):
+    """The bytes of t's cqsa_view; t must live on `device`."""
+    if t.device != device:
+        raise ValueError("all tensors of a call must live on one device")
+    s, n = t.stride(), t.shape
+    if len(s) != 4:
+        raise ValueError("tensors must be [B, L, H, d]")
+    if s[3] != 1:
+        raise ValueError("the last dimension must be contiguous")
+    code = _dtypes().get(t.dtype)
+    if code is None:
+        raise ValueError(f"tensors must be float32, float16 or bfloat16, got {t.dtype}")
+    return _VIEW.pack(t.data_ptr(), code, n[0], n[1], n[2], n[3], s[0], s[1], s[2])
+
+
+_dtype_table = {}
+
+
+def _dtypes():
+    if not _dtype_table:
+        torch = _torch()
+        _dtype_table.update({torch.float32: CQSA_F32, torch.float16: CQSA_F16, torch.bfloat16: CQSA_BF16})
+    return _dtype_table
+
+
 def _device_array(t, name, shape):
     """An int32 array that the C ABI takes as a bare pointer."""
     if t.dtype != _torch().int32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor on a GPU")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
 
 
-def _one_device(*ts):
-    d = ts[0].device
-    for t in ts:
-        if t is not None and t.device != d:
-            raise ValueError("all tensors of a call must live on one device")
-    return d
-
-
-def _enqueue(what, device, stream, call):
-    """call(stream) with `device` current, on `stream` or the device's current one."""
+def _raw_stream():
+    """The current stream of a device by its index, as an integer: torch's own short
+    way where it has one (it saves 1.5 us of every call), else by its stream object."""
     torch = _torch()
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _enqueue(what, device, stream, call)
+    return getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+        (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _enqueue(name, device, stream, *args):
+    """The call `name` with `device` current, on `stream` or the device's current one."""
+    cuda = _torch().cuda
+    if device.index != cuda.current_device():
+        with cuda.device(device):
+            return _enqueue(name, device, stream, *args)
     if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
-    _check(call(stream), what)
+        stream = _raw_stream()(device.index)
+    status = _call(name)(*args, stream)
+    if status != 0:
+        _check(status, name)
 
 
 class RotaryPlan:
@@ -487,17 +534,17 @@ def cqsa_rotary(plan, pos, x, y=None, inverse=False, stream=None):
     """Turn x (a [B, L, H, d] tensor, or a list of one or two: Q, or Q and K)
     into y (None: in place) by positions pos, int32 [axes, B, L].  inverse=True
     gives the gradient of x from that of y."""
-    xs = [x] if hasattr(x, "data_ptr") else list(x)
-    ys = xs if y is None else [y] if hasattr(y, "data_ptr") else list(y)
+    xs = (x,) if hasattr(x, "data_ptr") else x
+    ys = xs if y is None else (y,) if hasattr(y, "data_ptr") else y
     n = len(xs)
     if n not in (1, 2) or len(ys) != n:
         raise ValueError("one or two tensors, and as many results")
-    _device_array(pos, "pos", (plan.opts.n_axes, xs[0].shape[0], xs[0].shape[1]))
-    device = _one_device(pos, *xs, *ys)
-    vx = (cqsa_view * n)(*map(as_cqsa_view, xs))
-    vy = vx if ys is xs else (cqsa_view * n)(*map(as_cqsa_view, ys))
-    _enqueue("cqsa_rotary", device, stream,
-             lambda s: lib().cqsa_rotary(plan.handle, pos.data_ptr(), vx, vy, n, int(bool(inverse)), s))
+    shape = xs[0].shape
+    _device_array(pos, "pos", (plan.opts.n_axes, shape[0], shape[1]))
+    device = pos.device
+    vx = b"".join([_view(t, device) for t in xs])
+    vy = vx if ys is xs else b"".join([_view(t, device) for t in ys])
+    _enqueue("cqsa_rotary", device, stream, plan.handle, pos.data_ptr(), vx, vy, n, 1 if inverse else 0)
 
 
 def cqsa_cache_page_bytes(page_size, H, d):
@@ -523,7 +570,7 @@ class Cache4:
         if data.numel() != n_pages * per:
             raise ValueError(f"data must have {n_pages} x {per} bytes")
         self.n_pages, self.H, self.d, self.page_size = n_pages, H, d, page_size
-        self.data = data
+        self.data, self.device = data, data.device
         self.view = cqsa_cache(data.data_ptr(), n_pages, page_size, H, d)
 
 
@@ -542,7 +589,9 @@ class CacheBatch:
         if q_start is not None:
             _device_array(q_start, "q_start", (B + 1,))
         self.pages, self.lengths, self.q_start = pages, lengths, q_start
-        self.max_len, self.max_q, self.device = max_len, max_q, _one_device(pages, lengths, q_start)
+        self.max_len, self.max_q, self.device = max_len, max_q, pages.device
+        if lengths.device != self.device or (q_start is not None and q_start.device != self.device):
+            raise ValueError("all tensors of a batch must live on one device")
         self.view = cqsa_cache_batch(pages.data_ptr(), pages.stride(0) if B > 1 else n, lengths.data_ptr(),
                                      q_start.data_ptr() if q_start is not None else None, B, n,
                                      max_len, max_q)
@@ -553,16 +602,21 @@ class CacheBatch:
             return self.view
         v = cqsa_cache_batch.from_buffer_copy(self.view)
         if not self.max_len:
-            v.max_len = min(v.max_pages * cache.page_size, 2 ** 31 - 1)
+            v.max_len = min(v.max_pages * cache.page_size, 2 ** 30)
         if not self.max_q:
             v.max_q = t.shape[1]
         return v
 
 
-def _cache_move(what, cache, batch, K, V, stream):
-    device = _one_device(cache.data, batch.pages, K, V)
-    vk, vv, vb = as_cqsa_view(K), as_cqsa_view(V), batch._of(cache, K)
-    _enqueue(what, device, stream, lambda s: getattr(lib(), what)(cache.view, vb, vk, vv, s))
+def _cache_device(cache, batch):
+    if cache.device != batch.device:
+        raise ValueError("the cache and the batch must live on one device")
+    return cache.device
+
+
+def _cache_move(name, cache, batch, K, V, stream):
+    device = _cache_device(cache, batch)
+    _enqueue(name, device, stream, cache.view, batch._of(cache, K), _view(K, device), _view(V, device))
 
 
 def cqsa_cache_write(cache, batch, K, V, stream=None):
@@ -579,33 +633,35 @@ def cqsa_cache_attend_workspace(cache, batch, Q):
     """A workspace for cqsa_cache_attend with arguments of these sizes (a uint8
     tensor, or None where none is needed); calls that may overlap need their own."""
     n = ctypes.c_uint64()
-    _check(lib().cqsa_cache_attend_workspace(cache.view, batch._of(cache, Q), as_cqsa_view(Q), n),
+    device = _cache_device(cache, batch)
+    _check(_call("cqsa_cache_attend_workspace")(cache.view, batch._of(cache, Q), _view(Q, device), n),
            "cqsa_cache_attend_workspace")
-    return _torch().empty(n.value, dtype=_torch().uint8, device=Q.device) if n.value else None
+    return _torch().empty(n.value, dtype=_torch().uint8, device=device) if n.value else None
 
 
 def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, workspace=None, stream=None):
     """Attention of the call's rows Q over their sequences' cached tokens into O
     and, if given, LSE (fp32 [B, Hq, L], packed [1, Hq, T]).  workspace=None
     takes one from torch for this call."""
-    torch = _torch()
+    device = _cache_device(cache, batch)
+    vq, vo = _view(Q, device), _view(O, device)
+    lse = None
     if LSE is not None:
         want = (Q.shape[0], Q.shape[2], Q.shape[1])
-        if LSE.dtype != torch.float32 or not LSE.is_contiguous() or tuple(LSE.shape) != want:
-            raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {want}")
-    device = _one_device(cache.data, batch.pages, Q, O, LSE, workspace)
+        if LSE.dtype != _torch().float32 or LSE.device != device or not LSE.is_contiguous() or LSE.shape != want:
+            raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {want} on {device}")
+        lse = LSE.data_ptr()
+    space, size = None, 0
     if workspace is None:
         workspace = cqsa_cache_attend_workspace(cache, batch, Q)
         if workspace is not None and stream is not None:
-            workspace.record_stream(torch.cuda.ExternalStream(stream, device=device))
-    elif not workspace.is_contiguous():
-        raise ValueError("the workspace must be contiguous")
-    vq, vo, vb = as_cqsa_view(Q), as_cqsa_view(O), batch._of(cache, Q)
-    _enqueue("cqsa_cache_attend", device, stream,
-             lambda s: lib().cqsa_cache_attend(
-                 cache.view, vb, vq, vo, LSE.data_ptr() if LSE is not None else None,
-                 int(bool(causal)), float(scale), workspace.data_ptr() if workspace is not None else None,
-                 workspace.numel() * workspace.element_size() if workspace is not None else 0, s))
+            workspace.record_stream(_torch().cuda.ExternalStream(stream, device=device))
+    if workspace is not None:
+        if workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"the workspace must be a contiguous tensor on {device}")
+        space, size = workspace.data_ptr(), workspace.nbytes
+    _enqueue("cqsa_cache_attend", device, stream, cache.view, batch._of(cache, Q), vq, vo, lse,
+             1 if causal else 0, scale, space, size)
 
 
 def cqsa_set_timing(enable):

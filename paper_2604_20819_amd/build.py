@@ -28,6 +28,7 @@ SOURCES = [
     "rotary_driver.cpp", "cache_driver.cpp",
     "attn_fwd.hip", "merge.hip", "attn_bwd.hip", "stage.hip",
     "rotary.hip", "cache_quant.hip", "cache_attend.hip",
+    "cache_attend_many.hip",
 ]
 
 

@@ -57,12 +57,20 @@ struct AttendArgs {
 
 // How a call's rows and tokens are spread over work groups; by its sizes alone.
 struct AttendPlan {
-  int row_groups;  // of 16 rows, for each wave
+  int row_groups;  // of 16 rows, for each wave; 0: cache_attend_many
   int row_tiles;   // work groups over a sequence's and head's rows
   int splits;      // work groups over a sequence's tokens
+  int min_chunk;   // tiles that a split takes at least
 };
 // rows: the most that a sequence and key head has.
 AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
+
+// The kernel for many rows (of 16 bits): rows of a work group, 32 a wave, with two
+// waves on a SIMD where their registers fit; tokens of a tile (64 KB of LDS for
+// two of them); launch.
+constexpr int attend_many_rows(int d) { return d <= 128 ? 256 : 128; }
+constexpr int attend_many_tokens(int d) { return d <= 128 ? 64 : 32; }
+hipError_t launch_attend_many(cqsa_dtype dt, const AttendArgs& a, const AttendPlan& p, hipStream_t s);
 
 hipError_t launch_cache_write(cqsa_dtype dt, const CacheMoveArgs& a, hipStream_t s);
 hipError_t launch_cache_read(cqsa_dtype dt, const CacheMoveArgs& a, hipStream_t s);

@@ -12,6 +12,7 @@
 // + 4 q + r, which are the tokens whose scores the first product leaves it for
 // row c: the weights go from one product to the next in their registers.
 #include "cache_attend.hpp"
+#include <algorithm>
 
 namespace cqsa {
 
@@ -19,20 +20,21 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// What a wave reads of one tile.
-template <int DB>
-struct Tile {
-  static constexpr int NJ = (DB + 3) / 4;
-  u32x4 k[NJ][2];
-  uint32_t ke[NJ];
-  u32x2 v[DB], ve[DB];
-};
+// Waves a SIMD is to hold (and work groups a CU): as many as the registers
+// allow without spilling.  `parts` of the queries, blocks of 32 channels, groups
+// of 16 rows.
+constexpr int few_waves(int parts, int db, int nq) {
+  if (parts == 3) return db <= 3 ? 3 : (db <= 4 ? 2 : 1);
+  if (nq == 2) return 2;
+  if (parts == 2) return db <= 4 ? 3 : (db <= 6 ? 2 : 1);
+  return db <= 3 ? 4 : (db == 4 ? 3 : 2);
+}
 
 }  // namespace
 
 template <typename T, int DB, int NQ>
-__global__ void __launch_bounds__(64 * kWaves)
-    cache_attend_few(const AttendArgs a, int row_tiles, int splits) {
+__global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB, NQ)))
+    cache_attend_few(const AttendArgs a, int row_tiles, int splits, int min_chunk) {
   constexpr int D = 32 * DB, NJ = (DB + 3) / 4, QP = RowType<T>::kQuery, WP = RowType<T>::kWeight;
   constexpr int ROWS = 16 * NQ, QSTRIDE = 256 * NJ + 16;  // 16: rows on different banks
   constexpr int OSTRIDE = D + 4;
@@ -43,22 +45,33 @@ __global__ void __launch_bounds__(64 * kWaves)
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Work groups go round the XCDs in this order: neighbours are other heads and
+  // sequences, so that the splits of a sequence, the last of which may be
+  // short, do not load one XCD more than another.
   int id = blockIdx.x;
-  const int rt = id % row_tiles;
-  id /= row_tiles;
-  const int sp = id % splits;
-  id /= splits;
-  const int h = id % c.H, b = id / c.H;
+  const int h = id % c.H;
+  id /= c.H;
+  const int b = id % c.B;
+  id /= c.B;
+  const int rt = id % row_tiles, sp = id / row_tiles;
   const Seq s = sequence(c, b);
   const int rows = s.n * a.G, r0 = rt * ROWS;  // at most 2^31: checked on the host
   if (r0 >= rows) return;
   const int rlast = r0 + ROWS < rows ? r0 + ROWS - 1 : rows - 1;
   const int seen_min = seen_by(s, a.causal, r0 / a.G), seen_max = seen_by(s, a.causal, rlast / a.G);
   const int tiles = (seen_max + 31) >> 5;
-  const int chunk = (tiles + splits - 1) / splits;
+  const int even = (tiles + splits - 1) / splits, chunk = even > min_chunk ? even : min_chunk;
   const int t0 = sp * chunk, t1 = t0 + chunk < tiles ? t0 + chunk : tiles;
-
   const int64_t tb = c.q_start ? 0 : b;
+  if (splits > 1 && t0 >= t1) {  // nothing here: the join reads no more of it than this
+    if (tid < ROWS && r0 + tid < rows) {
+      const int r = r0 + tid;
+      const int64_t flat = (tb * a.Hq + h * a.G + r % a.G) * int64_t(c.rows) + s.row0 + r / a.G;
+      *(f32x2*)(a.part_ml + 2 * (flat * splits + sp)) = f32x2{-INFINITY, 0.f};
+    }
+    return;
+  }
+
   // queries, split into operands
   for (int u = tid; u < ROWS * 16 * NJ; u += 64 * kWaves) {
     const int r = u / (16 * NJ), e = 8 * (u % (16 * NJ));
@@ -117,24 +130,31 @@ __global__ void __launch_bounds__(64 * kWaves)
     const int blk = 4 * j + quarter < DB ? 4 * j + quarter : DB - 1;
     koff[j] = blk * 512 + col * 16;
   }
-  auto load = [&](Tile<DB>& x, int t, int32_t page) {
+  // What a wave holds of a tile: the keys are used first, so the next tile's are
+  // on their way while the values are, and the other way round.
+  u32x4 xk[NJ][2];
+  uint32_t xke[NJ];
+  u32x2 xv[DB], xve[DB];
+  auto load_keys = [&](int t, int32_t page) {
     const char* p = c.data + tile_at(c, page, h, t);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      x.k[j][0] = *(const u32x4*)(p + koff[j]);
-      x.k[j][1] = *(const u32x4*)(p + koff[j] + 256);
+      xk[j][0] = *(const u32x4*)(p + koff[j]);
+      xk[j][1] = *(const u32x4*)(p + koff[j] + 256);
       const int blk = 4 * j + quarter < DB ? 4 * j + quarter : DB - 1;
-      x.ke[j] = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * blk);
-    }
-#pragma unroll
-    for (int k = 0; k < DB; ++k) {
-      x.v[k] = *(const u32x2*)(p + 16 * D + k * 512 + col * 32 + quarter * 8);
-      x.ve[k] = *(const u32x2*)(p + 33 * D + quarter * 8 * DB + 8 * k);
+      xke[j] = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * blk);
     }
   };
-  auto compute = [&](Tile<DB>& x, int t) {
-    const bool mixed = 32 * t + 32 > seen_min;  // some row does not see all of the tile
-    f32x4 acc[NQ][2];
+  auto load_values = [&](int t, int32_t page) {
+    const char* p = c.data + tile_at(c, page, h, t);
+#pragma unroll
+    for (int k = 0; k < DB; ++k) {
+      xv[k] = *(const u32x2*)(p + 16 * D + k * 512 + col * 32 + quarter * 8);
+      xve[k] = *(const u32x2*)(p + 33 * D + quarter * 8 * DB + 8 * k);
+    }
+  };
+  f32x4 acc[NQ][2];
+  auto score = [&]() {
 #pragma unroll
     for (int n = 0; n < NQ; ++n) acc[n][0] = acc[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -143,13 +163,16 @@ __global__ void __launch_bounds__(64 * kWaves)
       for (int w = 0; w < 4; ++w)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const bf16x8 kk = decode8(x.k[j][u][w], scale_of(x.ke[j], u));
+          const bf16x8 kk = decode8(xk[j][u][w], scale_of(xke[j], u));
 #pragma unroll
           for (int n = 0; n < NQ; ++n)
 #pragma unroll
             for (int k = QP - 1; k >= 0; --k)
               acc[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qf[n][j][w][k], acc[n][u], 0, 0, 0);
         }
+  };
+  auto weigh = [&](int t) {
+    const bool mixed = 32 * t + 32 > seen_min;  // some row does not see all of the tile
     float p[NQ][8];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -197,11 +220,11 @@ __global__ void __launch_bounds__(64 * kWaves)
 #pragma unroll
       for (int k = 0; k < DB; ++k) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) x.ve[k][u] &= ~byte_mask(off[u]);
-        const uint32_t bad0 = nan_bytes(x.ve[k][0]), bad1 = nan_bytes(x.ve[k][1]);
+        for (int u = 0; u < 2; ++u) xve[k][u] &= ~byte_mask(off[u]);
+        const uint32_t bad0 = nan_bytes(xve[k][0]), bad1 = nan_bytes(xve[k][1]);
         if (__builtin_amdgcn_ballot_w64((bad0 | bad1) != 0u)) {
-          x.ve[k][0] &= ~byte_mask(bad0);
-          x.ve[k][1] &= ~byte_mask(bad1);
+          xve[k][0] &= ~byte_mask(bad0);
+          xve[k][1] &= ~byte_mask(bad1);
 #pragma unroll
           for (int n = 0; n < NQ; ++n) {
             bool hit = false;
@@ -222,9 +245,9 @@ __global__ void __launch_bounds__(64 * kWaves)
     for (int k = 0; k < DB; ++k) {
       u32x4 even, odd;
       uint32_t ev[2], od[2];
-      decode_quad(x.v[k][0], x.ve[k][0], ev, od);
+      decode_quad(xv[k][0], xve[k][0], ev, od);
       even[0] = ev[0], even[1] = ev[1], odd[0] = od[0], odd[1] = od[1];
-      decode_quad(x.v[k][1], x.ve[k][1], ev, od);
+      decode_quad(xv[k][1], xve[k][1], ev, od);
       even[2] = ev[0], even[3] = ev[1], odd[2] = od[0], odd[3] = od[1];
       const bf16x8 fe = __builtin_bit_cast(bf16x8, even), fo = __builtin_bit_cast(bf16x8, odd);
 #pragma unroll
@@ -237,36 +260,29 @@ __global__ void __launch_bounds__(64 * kWaves)
     }
   };
 
-  // Two tiles at a time in registers: one loads while the other is computed.
   int32_t pages = -1;
   int at = 64;  // place in the window
   auto next_page = [&](int t) {
+    if (t >= t1) return -1;
     if (at == 64) {
       pages = window(t);
       at = 0;
     }
     return __builtin_amdgcn_readlane(pages, at++);
   };
-  Tile<DB> x0, x1;
-  int t = t0 + wave;
-  int32_t p0 = -1, p1 = -1;
-  if (t < t1) {
-    p0 = next_page(t);
-    if (p0 >= 0) load(x0, t, p0);
+  int32_t page = next_page(t0 + wave);
+  if (page >= 0) {
+    load_keys(t0 + wave, page);
+    load_values(t0 + wave, page);
   }
-  while (t < t1) {
-    const int u = t + kWaves;
-    if (u < t1) {
-      p1 = next_page(u);
-      if (p1 >= 0) load(x1, u, p1);
-    }
-    if (p0 >= 0) compute(x0, t);
-    t = u + kWaves;
-    if (t < t1) {
-      p0 = next_page(t);
-      if (p0 >= 0) load(x0, t, p0);
-    }
-    if (u < t1 && p1 >= 0) compute(x1, u);
+  for (int t = t0 + wave; t < t1; t += kWaves) {
+    const int32_t next = next_page(t + kWaves);
+    const bool here = page >= 0;
+    if (here) score();
+    if (next >= 0) load_keys(t + kWaves, next);
+    if (here) weigh(t);
+    if (next >= 0) load_values(t + kWaves, next);
+    page = next;
   }
 
   // join the waves
@@ -339,37 +355,62 @@ __global__ void __launch_bounds__(64 * kWaves)
   }
 }
 
-// Joins the splits of a row: 16 rows a work group, 16 lanes each.
-template <typename T>
+// Joins the splits of a row: WPR waves a row, whose lanes share out its splits
+// and channels (4 a lane), so that a row of many splits is not a chain of
+// loads.
+template <typename T, int WPR>
 __global__ void __launch_bounds__(256) cache_attend_join(const AttendArgs a, int per_seq, int splits) {
+  constexpr int RPG = 4 / WPR;  // rows of a work group
   const CacheArgs& c = a.c;
-  const int sub = threadIdx.x & 15;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = wave % WPR;
   const int b = blockIdx.x / per_seq;
   const Seq s = sequence(c, b);
   const int64_t tb = c.q_start ? 0 : b;
   const int64_t rows = int64_t(s.n) * a.Hq;
-  for (int64_t i = int64_t(blockIdx.x % per_seq) * 16 + (threadIdx.x >> 4); i < rows;
-       i += int64_t(per_seq) * 16) {
-    const int tok = int(i / a.Hq), hq = int(i % a.Hq);
+  const int lanes = c.d / 4, ways = 64 / lanes;  // lanes of a split, splits at a time
+  const int way = lane / lanes, ch = 4 * (lane % lanes);
+  __shared__ float factor[4][kMaxSplits];
+  __shared__ f32x4 part[4][64];
+  for (int64_t i0 = int64_t(blockIdx.x % per_seq) * RPG; i0 < rows; i0 += int64_t(per_seq) * RPG) {
+    const int64_t i = i0 + wave / WPR;
+    const bool live = i < rows;
+    const int tok = live ? int(i / a.Hq) : 0, hq = live ? int(i % a.Hq) : 0;
     const int64_t flat = (tb * a.Hq + hq) * int64_t(c.rows) + s.row0 + tok;
     const float* ml = a.part_ml + 2 * flat * splits;
     float m = -INFINITY, l = 0.f;
-    for (int k = 0; k < splits; ++k) m = fmaxf(m, ml[2 * k]);
-    for (int k = 0; k < splits; ++k)
-      l += ml[2 * k + 1] * (ml[2 * k] == -INFINITY ? 1.f : fast_exp2(ml[2 * k] - m));
-    const float inv = l == 0.f ? 1.f : 1.f / l;
-    T* o = (T*)a.o.p + tb * a.o.b + int64_t(s.row0 + tok) * a.o.l + int64_t(hq) * a.o.h;
-    for (int ch = 4 * sub; ch < c.d; ch += 64) {
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      for (int k = 0; k < splits; ++k) {
-        const float f = ml[2 * k] == -INFINITY ? 1.f : fast_exp2(ml[2 * k] - m);
-        acc += *(const f32x4*)(a.part + (flat * splits + k) * c.d + ch) * f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (live) {
+      for (int k = lane; k < splits; k += 64) m = fmaxf(m, ml[2 * k]);
+      m = max_of_wave(m);
+      for (int k = lane; k < splits; k += 64) {
+        // a split that saw nothing wrote no more than these two
+        const float x = ml[2 * k], y = ml[2 * k + 1];
+        const float f = x == -INFINITY ? (y == 0.f ? 0.f : 1.f) : fast_exp2(x - m);
+        l += y * f;
+        factor[wave][k] = y == 0.f ? 0.f : f;
       }
+      l = sum_of_wave(l);
+      if (way < ways) {
+#pragma unroll 4
+        for (int k = sub * ways + way; k < splits; k += WPR * ways)
+          if (factor[wave][k] != 0.f)
+            acc += *(const f32x4*)(a.part + (flat * splits + k) * c.d + ch) * factor[wave][k];
+      }
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (live && sub == 0 && lane < lanes) {
+      acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < WPR; ++w)
+        for (int k = 0; k < ways; ++k) acc += part[wave + w][k * lanes + lane];
+      const float inv = l == 0.f ? 1.f : 1.f / l;
+      T* o = (T*)a.o.p + tb * a.o.b + int64_t(s.row0 + tok) * a.o.l + int64_t(hq) * a.o.h;
       typedef __attribute__((__vector_size__(4 * sizeof(T)))) T vec;
       *(vec*)(o + ch) = vec{T(acc[0] * inv), T(acc[1] * inv), T(acc[2] * inv), T(acc[3] * inv)};
+      if (a.lse && lane == 0)
+        a.lse[flat] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
     }
-    if (a.lse && sub == 0)
-      a.lse[flat] = l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(l)) * kLn2;
+    __syncthreads();
   }
 }
 
@@ -381,7 +422,9 @@ hipError_t launch_few(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   switch (a.c.d) {
 #define CQSA_FEW(DB)                                                                             \
   case 32 * DB:                                                                                  \
-    hipLaunchKernelGGL((cache_attend_few<T, DB, NQ>), grid, block, 0, s, a, p.row_tiles, p.splits); \
+    if constexpr (NQ == 1 || DB <= 4)                                                            \
+      hipLaunchKernelGGL((cache_attend_few<T, DB, NQ>), grid, block, 0, s, a, p.row_tiles, p.splits, \
+                       p.min_chunk); \
     break;
     CQSA_FEW(1)
     CQSA_FEW(2)
@@ -399,40 +442,93 @@ hipError_t launch_few(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_all(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  hipError_t e;
-  if constexpr (sizeof(T) == 2)
-    e = p.row_groups == 2 ? launch_few<T, 2>(a, p, s) : launch_few<T, 1>(a, p, s);
-  else
-    e = launch_few<T, 1>(a, p, s);
-  if (e != hipSuccess || p.splits == 1) return e;
+hipError_t launch_join(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   const int64_t rows = int64_t(a.c.q_start ? a.c.max_q : a.c.rows) * a.Hq;
-  int64_t per = (rows + 15) / 16;
+  const bool wide = p.splits > 8;
+  int64_t per = wide ? rows : (rows + 3) / 4;
   const int64_t most = (int64_t(1) << 23) / a.c.B;
   if (per > most) per = most;
-  hipLaunchKernelGGL((cache_attend_join<T>), dim3(unsigned(per * a.c.B)), dim3(256), 0, s, a, int(per),
-                     p.splits);
+  const dim3 grid(unsigned(per * a.c.B)), block(256);
+  if (wide)
+    hipLaunchKernelGGL((cache_attend_join<T, 4>), grid, block, 0, s, a, int(per), p.splits);
+  else
+    hipLaunchKernelGGL((cache_attend_join<T, 1>), grid, block, 0, s, a, int(per), p.splits);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_all(cqsa_dtype dt, const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+  hipError_t e;
+  if constexpr (sizeof(T) == 2)
+    e = p.row_groups == 0   ? launch_attend_many(dt, a, p, s)
+        : p.row_groups == 2 ? launch_few<T, 2>(a, p, s)
+                            : launch_few<T, 1>(a, p, s);
+  else
+    e = launch_few<T, 1>(a, p, s);
+  return e != hipSuccess || p.splits == 1 ? e : launch_join<T>(a, p, s);
 }
 
 }  // namespace
 
+// Which kernel, and how many work groups over a sequence's tokens.  Everything
+// goes by the work of a call, `units` of 16 rows by 32 tokens at the lengths'
+// bound, and by how the kernels' work groups fill the GPU.
 AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d) {
   AttendPlan p;
-  p.row_groups = rows > 16 && dt != CQSA_F32 && d <= 128 ? 2 : 1;
+  const int parts = dt == CQSA_F32 ? 3 : (dt == CQSA_F16 ? 2 : 1);
+  int64_t tiles = (max_len + 31) / 32;
+  const int64_t units = B * H * ((rows + 15) / 16) * tiles;
+  // The kernel for many rows decodes a tile once for 256 rows (128 from d =
+  // 160), but walks its tiles with a barrier each, so it has to have many of
+  // them.  us, few and many, bf16 d = 128, 8 key heads: 2^16 units (4096 tokens,
+  // 1024 rows) 36.6 and 37.6, 2^17 (4096, 2048) 51.6 and 53.3, 2^17 (32 times
+  // 2048, 128 rows) 72.8 and 49.7, 2^18 (8192, 2048) 97.8 and 84.0; d = 256: 2^18
+  // 218.6 and 229.4, 2^20 886.8 and 808.5.  In fp32 its three parts leave no
+  // registers for a second wave (d = 128: 2^20 units 741.7 and 727.0, d = 256
+  // 1757 and 2450), so it is not built for that.
+  const bool many = dt != CQSA_F32 && rows > 64 && units >= (d <= 128 ? 1 << 17 : 1 << 19);
+  if (many) {
+    p.row_groups = 0;
+    p.row_tiles = int((rows + attend_many_rows(d) - 1) / attend_many_rows(d));
+    // one work group a CU: the number of splits whose rounds of 256 are the
+    // shortest in all, with 6 tiles' time for a round's start and end
+    tiles = (max_len + attend_many_tokens(d) - 1) / attend_many_tokens(d);
+    const int64_t groups = B * H * p.row_tiles;
+    int64_t best = 0;
+    p.splits = 1;
+    for (int s = 1; s <= 16 && (s == 1 || tiles / s >= 8); ++s) {
+      const int64_t cost = (groups * s + 255) / 256 * ((tiles + s - 1) / s + 6);
+      if (s == 1 || cost < best) best = cost, p.splits = s;
+    }
+    p.min_chunk = 8;
+    return p;
+  }
+  // Two groups of 16 rows a wave share a tile's decoding, one leaves twice the
+  // work groups: 2^13 units 13.0 us with one and 13.6 with two, 2^15 27.9 and
+  // 25.8, 2^18 126.4 and 97.8 (bf16, d = 128).
+  p.row_groups = dt != CQSA_F32 && d <= 128 && rows > 16 && units >= 1 << 15 ? 2 : 1;
   p.row_tiles = int((rows + 16 * p.row_groups - 1) / (16 * p.row_groups));
-  const int64_t tiles = (max_len + 31) / 32, groups = B * H * p.row_tiles;
-  int64_t s = 1;
-  if (groups < 1024) s = (1024 + groups - 1) / groups;
-  if (s > tiles / 8) s = tiles / 8;
-  p.splits = int(s < 1 ? 1 : s);
+  const int64_t groups = B * H * p.row_tiles;
+  const int64_t slots = 256 * few_waves(parts, d / 32, p.row_groups);
+  const int64_t once = (groups * tiles + slots - 1) / slots;  // tiles that fill the GPU once
+  // One sequence: equal parts, all at once (2^20 tokens, 8 heads: 96 splits 204
+  // us, 64 236, 128 253).  Several: their lengths may differ, so parts of a
+  // quarter of that even them out (64 of up to 16384: 136.8, in one round 161),
+  // but no smaller than 32 tiles where these fill the GPU, else 16 (16 of up to
+  // 8192 tokens, fp16: 32 tiles 22.8, 16 25.9).
+  int64_t chunk = std::max<int64_t>(16, once);
+  if (B > 1) chunk = std::max<int64_t>({16, std::min<int64_t>(32, once), (once + 3) / 4});
+  // up to 48 tiles a second launch costs more than it spares (1000 tokens: 10.0 and 12.0 us)
+  if (tiles <= 48) chunk = 48;
+  p.splits = int(std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, (tiles + chunk - 1) / chunk)));
+  p.min_chunk = int(std::min<int64_t>(chunk, 1 << 30));
   return p;
 }
 
 hipError_t launch_cache_attend(cqsa_dtype dt, const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  if (dt == CQSA_BF16) return launch_all<__bf16>(a, p, s);
-  if (dt == CQSA_F16) return launch_all<_Float16>(a, p, s);
-  return launch_all<float>(a, p, s);
+  if (dt == CQSA_BF16) return launch_all<__bf16>(dt, a, p, s);
+  if (dt == CQSA_F16) return launch_all<_Float16>(dt, a, p, s);
+  return launch_all<float>(dt, a, p, s);
 }
 
 }  // namespace cqsa

@@ -17,6 +17,8 @@
 
 namespace cqsa {
 
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+
 // Rows of dtype T: bf16 parts of a query, and of a weight.
 template <typename T>
 struct RowType;
@@ -33,6 +35,7 @@ struct RowType<float> {
   static constexpr int kQuery = 3, kWeight = 3;
 };
 
+constexpr int kMaxSplits = 512;
 constexpr float kLn2 = 0.69314718055994530942f;
 // A tile keeps its row's shift while no score is more than this above it (in
 // powers of two): the weights then stay under 2^8, far from fp32's and bf16's
@@ -132,7 +135,18 @@ __device__ __forceinline__ float sum_of_quarters(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// Tokens that a row sees, and those that the first and the last of some rows see.
+__device__ __forceinline__ float max_of_wave(float x) {
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) x = fmaxf(x, __shfl_xor(x, k));
+  return x;
+}
+__device__ __forceinline__ float sum_of_wave(float x) {
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
+  return x;
+}
+
+// Tokens that a row sees.
 __device__ __forceinline__ int seen_by(const Seq& s, int causal, int token) {
   const int v = causal ? s.len - s.n + token + 1 : s.len;
   return v < 0 ? 0 : v;

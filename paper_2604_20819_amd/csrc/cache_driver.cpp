@@ -40,8 +40,8 @@ cqsa_status check_batch(const cqsa_cache* c, const cqsa_cache_batch* b, const st
   if (b->B < 0 || b->B > (1 << 20)) return fail(CQSA_ERR_INVALID_ARG, what + "batch.B must be in [0, 2^20]");
   if (b->max_pages < 0 || b->pages_stride < b->max_pages)
     return fail(CQSA_ERR_INVALID_ARG, what + "pages_stride must be max_pages or more, and that 0 or more");
-  if (b->max_len < 0 || b->max_len > int64_t(b->max_pages) * c->page_size)
-    return fail(CQSA_ERR_INVALID_ARG, what + "max_len must be in [0, max_pages * page_size]");
+  if (b->max_len < 0 || b->max_len > int64_t(b->max_pages) * c->page_size || b->max_len > (1 << 30))
+    return fail(CQSA_ERR_INVALID_ARG, what + "max_len must be in [0, max_pages * page_size], at most 2^30");
   return CQSA_OK;
 }
 

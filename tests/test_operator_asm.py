@@ -7,7 +7,7 @@ import pytest
 
 from paper_2604_20819_amd import build
 
-SOURCES = ["rotary.hip", "cache_quant.hip", "cache_attend.hip"]
+SOURCES = ["rotary.hip", "cache_quant.hip", "cache_attend.hip", "cache_attend_many.hip"]
 
 
 @pytest.fixture(scope="module")
