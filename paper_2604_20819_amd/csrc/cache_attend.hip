@@ -35,7 +35,7 @@ constexpr int few_waves(int parts, int db, int nq) {
 template <typename T, int DB, int NQ>
 __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB, NQ)))
     cache_attend_few(const AttendArgs a, int row_tiles, int splits, int min_chunk) {
-  constexpr int D = 32 * DB, NJ = (DB + 3) / 4, QP = RowType<T>::kQuery, WP = RowType<T>::kWeight;
+  constexpr int D = 32 * DB, NJ = (DB + 3) / 4, QP = RowType<T>::kQuery, WP = NQ == 1 ? RowType<T>::kWeightFew : RowType<T>::kWeight;
   constexpr int ROWS = 16 * NQ, QSTRIDE = 256 * NJ + 16;  // 16: rows on different banks
   constexpr int OSTRIDE = D + 4;
   constexpr int QBYTES = QP * ROWS * QSTRIDE, OBYTES = kWaves * 16 * OSTRIDE * 4;

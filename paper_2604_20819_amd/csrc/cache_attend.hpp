@@ -4,8 +4,11 @@
 // bf16 holds every cached value exactly, so both products are bf16 matrix
 // products with fp32 sums; what has more bits than a bf16 enters them in parts
 // that add up to it: queries of fp16 in 2, of fp32 in 3, which makes the scores'
-// products exact; weights in 1 for bf16 rows, whose result has no more bits,
-// in 2 for fp16 and 3 for fp32.  v_mfma_scale_f32_16x16x128_f8f6f4 would take
+// products exact; weights in 2 for fp16 and 3 for fp32, and for bf16 rows in 2
+// where there are few and the cache's bytes bound the call (2 to 3 % of its
+// time), else in 1, which adds to a result that is rounded to bf16 anyway about
+// as much as that rounding (error of the result against 64 bits 2.4e-3 with
+// one part, 1.7e-3 with two; two take 10 to 15 % more from 17 rows on).  v_mfma_scale_f32_16x16x128_f8f6f4 would take
 // the keys' codes and exponents as they are and save their decoding, but it
 // drops bits of products that lie some 11 binades below a sum's largest (a
 // score off by 2^-13 of its largest product, measured), and queries in e4m3
@@ -19,20 +22,21 @@ namespace cqsa {
 
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
 
-// Rows of dtype T: bf16 parts of a query, and of a weight.
+// Rows of dtype T: bf16 parts of a query, and of a weight with many and with few
+// rows.
 template <typename T>
 struct RowType;
 template <>
 struct RowType<__bf16> {
-  static constexpr int kQuery = 1, kWeight = 1;
+  static constexpr int kQuery = 1, kWeight = 1, kWeightFew = 2;
 };
 template <>
 struct RowType<_Float16> {
-  static constexpr int kQuery = 2, kWeight = 2;
+  static constexpr int kQuery = 2, kWeight = 2, kWeightFew = 2;
 };
 template <>
 struct RowType<float> {
-  static constexpr int kQuery = 3, kWeight = 3;
+  static constexpr int kQuery = 3, kWeight = 3, kWeightFew = 3;
 };
 
 constexpr int kMaxSplits = 512;

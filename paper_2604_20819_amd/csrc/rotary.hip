@@ -14,40 +14,41 @@ namespace cqsa {
 
 namespace {
 
+// Two runs of 8 elements.  A run of fp32 is two vectors, `far` elements apart,
+// so that every load and store of neighbouring lanes covers whole lines.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* v) {
-  typedef __attribute__((__vector_size__(8 * sizeof(T)))) T vec;
-  const vec x = *(const vec*)p;
+struct Vec16 {
+  static constexpr int N = 16 / sizeof(T), V = 8 / N;  // of a 16-byte vector, vectors of a run
+  typedef __attribute__((__vector_size__(16))) T vec;
+  vec x[2 * V];
+  __device__ __forceinline__ void load(const T* p, const T* q, uint32_t far) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = float(x[i]);
-}
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* v) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const f32x4 x = ((const f32x4*)p)[j];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[4 * j + i] = x[i];
+    for (int i = 0; i < V; ++i) x[i] = *(const vec*)(p + i * far), x[V + i] = *(const vec*)(q + i * far);
   }
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float* v) {
-  typedef __attribute__((__vector_size__(8 * sizeof(T)))) T vec;
-  vec x;
+  template <bool LINES>
+  __device__ __forceinline__ void store(T* p, T* q, uint32_t far) const {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = T(v[i]);
-  *(vec*)p = x;
-}
-template <>
-__device__ __forceinline__ void store8<float>(float* p, const float* v) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    f32x4 x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = v[4 * j + i];
-    ((f32x4*)p)[j] = x;
+    for (int i = 0; i < V; ++i) {
+      vec* const a = (vec*)(p + i * far);
+      vec* const b = (vec*)(q + i * far);
+      if constexpr (LINES) {
+        __builtin_nontemporal_store(x[i], a);
+        __builtin_nontemporal_store(x[V + i], b);
+      } else {
+        *a = x[i];
+        *b = x[V + i];
+      }
+    }
   }
-}
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = float(x[i / N][i % N]);
+  }
+  __device__ __forceinline__ void set(const float* f) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i / N][i % N] = T(f[i]);
+  }
+};
 
 // Sine and cosine of v * 2^-32 turns.
 __device__ __forceinline__ void sin_cos_turns(uint32_t v, float* s, float* c) {
@@ -66,9 +67,16 @@ __device__ __forceinline__ void sin_cos_turns(uint32_t v, float* s, float* c) {
 }  // namespace
 
 // One thread turns a chunk of 8 pairs of the heads part, part + parts, ... of
-// one row; the chunk's angles are computed once for all of them.
-template <typename T, bool ADJACENT>
+// one row; the chunk's angles, some 300 instructions, are computed once for
+// all of them.  rotary_batch heads are read before the first of them is written:
+// 8 of 16 bits, 4 of 32 (32768 rows of 32 heads, bf16, d = 128: 83 us with 8, 97
+// with 4; 131072 of 16, fp32, d = 64: 222 and 216).  Where 8 lanes side by side
+// write a line of 128 bytes at once, they write it past the caches, which it
+// would only pass through (the same rows: 97 and 149 us); written in halves, it
+// is better gathered there (fp32, d = 64: 216 and 197).
+template <typename T, bool ADJACENT, bool LINES>
 __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
+  constexpr int BATCH = rotary_batch(sizeof(T));
   const uint32_t i = blockIdx.x * 256 + threadIdx.x;
   if (i >= a.n) return;
   const uint32_t u = i % a.units, part = i / a.units % a.parts;
@@ -76,49 +84,66 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
   const int64_t b = row / a.L, l = row % a.L;
   const bool turned = u < a.chunks;
   float sn[8], cs[8];
-  // elements of the chunk's first and second eight
-  const uint32_t e0 = turned && !ADJACENT ? 8 * u : 16 * u;
-  const uint32_t e1 = turned && !ADJACENT ? 8 * u + a.pairs : 16 * u + 8;
+  // The chunk's two runs of 8 elements: 8 pairs across the runs, or 4 within each.
+  constexpr uint32_t N = Vec16<T>::N;
+  const uint32_t e0 = turned ? N * u : 16 * u, e1 = e0 + (turned ? a.pairs : 8);
+  const uint32_t far = turned ? a.pairs / 2 : N;
   if (turned) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int64_t p = a.pos[a.tab.axis[8 * u + j] * a.rows + row];
-      sin_cos_turns(uint32_t((uint64_t(p) * a.tab.turn[8 * u + j]) >> 32), &sn[j], &cs[j]);
+      // of the run's elements e (and of those in the other run that are its like)
+      const uint32_t k = ADJACENT ? 2 * (j % 4) : j, e = N * u + k / N * far + k % N;
+      const uint32_t pair = ADJACENT ? (j / 4 * a.pairs + e) / 2 : e;
+      const int64_t p = a.pos[a.tab.axis[pair] * a.rows + row];
+      sin_cos_turns(uint32_t((uint64_t(p) * a.tab.turn[pair]) >> 32), &sn[j], &cs[j]);
       if (a.inverse) sn[j] = -sn[j];
     }
   }
-  for (uint32_t hv = part; hv < a.H; hv += a.parts) {
-    const int k = hv >= a.H0;
-    const RotaryArgs::Tensor& t = a.t[k];
-    const int64_t h = hv - (k ? a.H0 : 0);
-    const T* x = (const T*)t.x + b * t.x_b + l * t.x_l + h * t.x_h;
-    T* y = (T*)t.y + b * t.y_b + l * t.y_l + h * t.y_h;
-    float v[16], w[16];
-    load8<T>(x + e0, v);
-    load8<T>(x + e1, v + 8);
-    if (turned) {
+  for (uint32_t h0 = part; h0 < a.H; h0 += BATCH * a.parts) {
+    Vec16<T> v[BATCH];
+    T* y[BATCH];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int p = ADJACENT ? 2 * j : j, q = ADJACENT ? 2 * j + 1 : j + 8;
-        w[p] = v[p] * cs[j] - v[q] * sn[j];
-        w[q] = v[q] * cs[j] + v[p] * sn[j];
+    for (int k = 0; k < BATCH; ++k) {
+      const uint32_t hv = h0 + k * a.parts;
+      if (hv < a.H) {
+        const RotaryArgs::Tensor& t = a.t[hv >= a.H0];
+        const int64_t h = hv - (hv >= a.H0 ? a.H0 : 0);
+        const T* x = (const T*)t.x + b * t.x_b + l * t.x_l + h * t.x_h;
+        y[k] = (T*)t.y + b * t.y_b + l * t.y_l + h * t.y_h;
+        v[k].load(x + e0, x + e1, far);
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) w[j] = v[j];
     }
-    store8<T>(y + e0, w);
-    store8<T>(y + e1, w + 8);
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      if (h0 + k * a.parts < a.H) {
+        if (turned) {
+          float x[16], w[16];
+          v[k].get(x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int p = ADJACENT ? 2 * j : j, q = ADJACENT ? 2 * j + 1 : j + 8;
+            w[p] = x[p] * cs[j] - x[q] * sn[j];
+            w[q] = x[q] * cs[j] + x[p] * sn[j];
+          }
+          v[k].set(w);
+        }
+        v[k].template store<LINES>(y[k] + e0, y[k] + e1, far);
+      }
   }
 }
 
 hipError_t launch_rotary(cqsa_dtype dt, bool adjacent, const RotaryArgs& a, hipStream_t s) {
   const dim3 grid((a.n + 255) / 256), block(256);
+  const bool lines = a.chunks % 8 == 0;
 #define CQSA_ROT(T)                                                             \
-  if (adjacent)                                                                 \
-    hipLaunchKernelGGL((rotary_kernel<T, true>), grid, block, 0, s, a);         \
+  if (adjacent && lines)                                                        \
+    hipLaunchKernelGGL((rotary_kernel<T, true, true>), grid, block, 0, s, a);   \
+  else if (adjacent)                                                            \
+    hipLaunchKernelGGL((rotary_kernel<T, true, false>), grid, block, 0, s, a);  \
+  else if (lines)                                                               \
+    hipLaunchKernelGGL((rotary_kernel<T, false, true>), grid, block, 0, s, a);  \
   else                                                                          \
-    hipLaunchKernelGGL((rotary_kernel<T, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((rotary_kernel<T, false, false>), grid, block, 0, s, a);
   if (dt == CQSA_BF16) {
     CQSA_ROT(__bf16)
   } else if (dt == CQSA_F16) {

@@ -37,6 +37,9 @@ struct RotaryArgs {
   RotaryTable tab;
 };
 
+// Heads that a thread reads at a time.
+constexpr int rotary_batch(int elem_bytes) { return 16 / elem_bytes; }
+
 hipError_t launch_rotary(cqsa_dtype dt, bool adjacent, const RotaryArgs& a, hipStream_t s);
 
 }  // namespace cqsa
