@@ -6,11 +6,13 @@
 // unnormalised result each, which are joined at the end through LDS; a long
 // sequence is split over `splits` work groups, joined by a second kernel.
 //
-// Per tile, lane (q, c) = (lane / 16, lane % 16) holds for the keys 16 t + c
-// (t = 0, 1) the blocks 4 j + q (the sums over d take them in this order), and
-// for the values the channels 2 c and 2 c + 1 of every block at the tokens 16 t
-// + 4 q + r, which are the tokens whose scores the first product leaves it for
-// row c: the weights go from one product to the next in their registers.
+// Per tile, lane (q, c) = (lane / 16, lane % 16) holds keys 16 t + c (t = 0, 1):
+// where d is a multiple of 128 the blocks 4 j + q, 16 bytes of codes each (the
+// sums over d take their terms in this order), else 8 elements of every block,
+// 4 bytes each, since a fourth of the lanes would hold no block.  Of the values
+// it holds the channels 2 c and 2 c + 1 of every block at the tokens 16 t + 4 q
+// + r, which are the tokens whose scores the first product leaves it for row c:
+// the weights go from one product to the next in their registers.
 #include "cache_attend.hpp"
 #include <algorithm>
 
@@ -24,10 +26,10 @@ constexpr int kWaves = 4;
 // allow without spilling.  `parts` of the queries, blocks of 32 channels, groups
 // of 16 rows.
 constexpr int few_waves(int parts, int db, int nq) {
-  if (parts == 3) return db <= 3 ? 3 : (db <= 4 ? 2 : 1);
-  if (nq == 2) return 2;
-  if (parts == 2) return db <= 4 ? 3 : (db <= 6 ? 2 : 1);
-  return db <= 3 ? 4 : (db == 4 ? 3 : 2);
+  if (nq == 2) return parts == 1 ? (db == 1 ? 4 : (db == 2 ? 3 : 2)) : (db <= 2 ? 3 : 2);
+  if (parts == 1) return db <= 3 ? 4 : (db <= 5 ? 3 : 2);
+  if (parts == 2) return db <= 2 ? 4 : (db <= 4 ? 3 : 2);
+  return db <= 2 ? 4 : (db == 3 ? 3 : (db <= 6 ? 2 : 1));
 }
 
 }  // namespace
@@ -35,8 +37,9 @@ constexpr int few_waves(int parts, int db, int nq) {
 template <typename T, int DB, int NQ>
 __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB, NQ)))
     cache_attend_few(const AttendArgs a, int row_tiles, int splits, int min_chunk) {
-  constexpr int D = 32 * DB, NJ = (DB + 3) / 4, QP = RowType<T>::kQuery, WP = NQ == 1 ? RowType<T>::kWeightFew : RowType<T>::kWeight;
-  constexpr int ROWS = 16 * NQ, QSTRIDE = 256 * NJ + 16;  // 16: rows on different banks
+  constexpr bool WIDE = DB % 4 == 0;  // whole blocks a lane
+  constexpr int D = 32 * DB, QP = RowType<T>::kQuery, WP = NQ == 1 ? RowType<T>::kWeightFew : RowType<T>::kWeight;
+  constexpr int ROWS = 16 * NQ, QSTRIDE = 2 * D + 16;  // 16: rows on different banks
   constexpr int OSTRIDE = D + 4;
   constexpr int QBYTES = QP * ROWS * QSTRIDE, OBYTES = kWaves * 16 * OSTRIDE * 4;
   __shared__ __attribute__((aligned(16))) char lds[QBYTES > OBYTES ? QBYTES : OBYTES];
@@ -72,11 +75,69 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
     return;
   }
 
+  // pages of this wave's next 64 tiles, one a lane
+  auto window = [&](int t) {
+    const int u = t + kWaves * lane;
+    return u < t1 ? int32_t(page_of(c, b, u)) : -1;
+  };
+  // What a wave holds of a tile: the keys are used first, so the next tile's are
+  // on their way while the values are, and the other way round.
+  uint32_t xk[DB][2];               // step w's 8 codes of tokens c and 16 + c
+  uint32_t xke[WIDE ? DB / 4 : DB];  // and their exponents
+  u32x2 xv[DB], xve[DB];
+  auto load_keys = [&](int t, int32_t page) {
+    const char* p = c.data + tile_at(c, page, h, t);
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int j = 0; j < DB / 4; ++j) {
+        const int blk = 4 * j + quarter;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const u32x4 x = *(const u32x4*)(p + blk * 512 + (16 * u + col) * 16);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) xk[4 * j + w][u] = x[w];
+        }
+        xke[j] = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * blk);
+      }
+    } else {
+#pragma unroll
+      for (int w = 0; w < DB; ++w) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          xk[w][u] = *(const uint32_t*)(p + w * 512 + (16 * u + col) * 16 + 4 * quarter);
+        xke[w] = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * w);
+      }
+    }
+  };
+  auto load_values = [&](int t, int32_t page) {
+    const char* p = c.data + tile_at(c, page, h, t);
+#pragma unroll
+    for (int k = 0; k < DB; ++k) {
+      xv[k] = *(const u32x2*)(p + 16 * D + k * 512 + col * 32 + quarter * 8);
+      xve[k] = *(const u32x2*)(p + 33 * D + quarter * 8 * DB + 8 * k);
+    }
+  };
+  int32_t pages = -1;
+  int at = 64;  // place in the window
+  auto next_page = [&](int t) {
+    if (t >= t1) return -1;
+    if (at == 64) {
+      pages = window(t);
+      at = 0;
+    }
+    return __builtin_amdgcn_readlane(pages, at++);
+  };
+  int32_t page = next_page(t0 + wave);  // on its way while the queries come
+  if (page >= 0) {
+    load_keys(t0 + wave, page);
+    load_values(t0 + wave, page);
+  }
+
   // queries, split into operands
-  for (int u = tid; u < ROWS * 16 * NJ; u += 64 * kWaves) {
-    const int r = u / (16 * NJ), e = 8 * (u % (16 * NJ));
+  for (int u = tid; u < ROWS * 4 * DB; u += 64 * kWaves) {
+    const int r = u / (4 * DB), e = 8 * (u % (4 * DB));
     float v[8];
-    if (r0 + r < rows && e < D) {
+    if (r0 + r < rows) {
       const int tok = (r0 + r) / a.G, g = (r0 + r) % a.G;
       load_row8<T>((const T*)a.q.p + tb * a.q.b + int64_t(s.row0 + tok) * a.q.l +
                        int64_t(h * a.G + g) * a.q.h + e, v);
@@ -90,17 +151,17 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
     for (int k = 0; k < QP; ++k) *(bf16x8*)(lds + (k * ROWS + r) * QSTRIDE + 2 * e) = part[k];
   }
   __syncthreads();
-  bf16x8 qf[NQ][NJ][4][QP];
+  // step w of the scores' product: 8 elements of each of 4 blocks, or a block
+  bf16x8 qf[NQ][DB][QP];
 #pragma unroll
   for (int n = 0; n < NQ; ++n)
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+    for (int w = 0; w < DB; ++w)
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-#pragma unroll
-        for (int k = 0; k < QP; ++k)
-          qf[n][j][w][k] = *(const bf16x8*)(lds + (k * ROWS + 16 * n + col) * QSTRIDE +
-                                            2 * (32 * (4 * j + quarter) + 8 * w));
+      for (int k = 0; k < QP; ++k) {
+        const int e = WIDE ? 32 * (4 * (w / 4) + quarter) + 8 * (w % 4) : 32 * w + 8 * quarter;
+        qf[n][w][k] = *(const bf16x8*)(lds + (k * ROWS + 16 * n + col) * QSTRIDE + 2 * e);
+      }
   int seen[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
@@ -118,58 +179,21 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
     for (int k = 0; k < DB; ++k) o[n][k][0] = o[n][k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // pages of this wave's next 64 tiles, one a lane
-  auto window = [&](int t) {
-    const int u = t + kWaves * lane;
-    return u < t1 ? int32_t(page_of(c, b, u)) : -1;
-  };
-  int koff[NJ];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    // a block past d reads the last one's bytes again; its query is 0
-    const int blk = 4 * j + quarter < DB ? 4 * j + quarter : DB - 1;
-    koff[j] = blk * 512 + col * 16;
-  }
-  // What a wave holds of a tile: the keys are used first, so the next tile's are
-  // on their way while the values are, and the other way round.
-  u32x4 xk[NJ][2];
-  uint32_t xke[NJ];
-  u32x2 xv[DB], xve[DB];
-  auto load_keys = [&](int t, int32_t page) {
-    const char* p = c.data + tile_at(c, page, h, t);
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      xk[j][0] = *(const u32x4*)(p + koff[j]);
-      xk[j][1] = *(const u32x4*)(p + koff[j] + 256);
-      const int blk = 4 * j + quarter < DB ? 4 * j + quarter : DB - 1;
-      xke[j] = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * blk);
-    }
-  };
-  auto load_values = [&](int t, int32_t page) {
-    const char* p = c.data + tile_at(c, page, h, t);
-#pragma unroll
-    for (int k = 0; k < DB; ++k) {
-      xv[k] = *(const u32x2*)(p + 16 * D + k * 512 + col * 32 + quarter * 8);
-      xve[k] = *(const u32x2*)(p + 33 * D + quarter * 8 * DB + 8 * k);
-    }
-  };
   f32x4 acc[NQ][2];
   auto score = [&]() {
 #pragma unroll
     for (int n = 0; n < NQ; ++n) acc[n][0] = acc[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+    for (int w = 0; w < DB; ++w)
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 kk = decode8(xk[w][u], scale_of(xke[WIDE ? w / 4 : w], u));
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bf16x8 kk = decode8(xk[j][u][w], scale_of(xke[j], u));
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
-          for (int n = 0; n < NQ; ++n)
-#pragma unroll
-            for (int k = QP - 1; k >= 0; --k)
-              acc[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qf[n][j][w][k], acc[n][u], 0, 0, 0);
-        }
+          for (int k = QP - 1; k >= 0; --k)
+            acc[n][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qf[n][w][k], acc[n][u], 0, 0, 0);
+      }
   };
   auto weigh = [&](int t) {
     const bool mixed = 32 * t + 32 > seen_min;  // some row does not see all of the tile
@@ -260,21 +284,6 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
     }
   };
 
-  int32_t pages = -1;
-  int at = 64;  // place in the window
-  auto next_page = [&](int t) {
-    if (t >= t1) return -1;
-    if (at == 64) {
-      pages = window(t);
-      at = 0;
-    }
-    return __builtin_amdgcn_readlane(pages, at++);
-  };
-  int32_t page = next_page(t0 + wave);
-  if (page >= 0) {
-    load_keys(t0 + wave, page);
-    load_values(t0 + wave, page);
-  }
   for (int t = t0 + wave; t < t1; t += kWaves) {
     const int32_t next = next_page(t + kWaves);
     const bool here = page >= 0;
@@ -513,13 +522,15 @@ AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa
   const int64_t once = (groups * tiles + slots - 1) / slots;  // tiles that fill the GPU once
   // One sequence: equal parts, all at once (2^20 tokens, 8 heads: 96 splits 204
   // us, 64 236, 128 253).  Several: their lengths may differ, so parts of a
-  // quarter of that even them out (64 of up to 16384: 136.8, in one round 161),
-  // but no smaller than 32 tiles where these fill the GPU, else 16 (16 of up to
-  // 8192 tokens, fp16: 32 tiles 22.8, 16 25.9).
-  int64_t chunk = std::max<int64_t>(16, once);
-  if (B > 1) chunk = std::max<int64_t>({16, std::min<int64_t>(32, once), (once + 3) / 4});
-  // up to 48 tiles a second launch costs more than it spares (1000 tokens: 10.0 and 12.0 us)
-  if (tiles <= 48) chunk = 48;
+  // quarter of that even them out (64 of up to 16384 tokens: 139, in one round
+  // 161).  A part is no smaller than what its start, its end and the join cost:
+  // 8 tiles for one sequence (1000 tokens: 9.7 us, unsplit 10.7; 4096: 10.0, with
+  // 32 tiles 13.6), 16 to 24 for several (16 of up to 8192: 24 tiles 22.6, 16
+  // 25.3), and 96 where the work groups without any split fill half of the GPU
+  // (64 of up to 2048: unsplit 24.3, 32 tiles 27.5).
+  const int64_t least = 2 * groups >= slots ? 96 : (B == 1 ? 8 : std::max<int64_t>(16, std::min<int64_t>(24, once)));
+  int64_t chunk = std::max<int64_t>(least, B > 1 ? (once + 3) / 4 : once);
+  if (tiles <= 16) chunk = 16;
   p.splits = int(std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, (tiles + chunk - 1) / chunk)));
   p.min_chunk = int(std::min<int64_t>(chunk, 1 << 30));
   return p;
