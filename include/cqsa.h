@@ -428,9 +428,11 @@ void cqsa_rotary_destroy(cqsa_rotary_t* plan); /* NULL is a no-op */
 /* y[k] = x[k] with every pair (a, b) of every token's every head turned by the
  * pair's angle w = pos_scale * pos * (its turn a position):
  * (a cos w - b sin w, b cos w + a sin w).  inverse = 1 turns by -w: the
- * gradient of x[k] from that of y[k].  n = 1 or 2 tensors (Q, or Q and K) are
- * turned in one launch; they share B, L, d and the dtype.  y[k] may be x[k]
- * itself (same data and strides).  pos: int32 [n_axes, B, L] in device memory,
+ * gradient of x[k] from that of y[k].  n = 1 or 2 tensors (Q, or Q and K) of
+ * at most 2^20 heads together are turned in one launch; they share B, L, d and
+ * the dtype.  y[k] may be x[k] itself (same data and strides); else the memory
+ * that it spans must not meet what x[k] spans, nor its elements the other
+ * tensor's.  pos: int32 [n_axes, B, L] in device memory,
  * any value: angles are reduced in 64-bit fixed point (2^-64 turns a position,
  * so 2^-33 turns at the farthest), and the products are fp32, rounded once. */
 cqsa_status cqsa_rotary(const cqsa_rotary_t* plan, const int32_t* pos, const cqsa_view* x,
@@ -502,7 +504,7 @@ cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* bat
 /* Attention of the call's rows Q (H_q heads, a multiple of the cache's H; head h reads the
  * cache's head h / (H_q / H)) over their sequences' cached tokens: with causal = 1 row i of
  * sequence b sees positions 0 ... lengths[b] - n_b + i, with 0 all of them.  O: Q's shape
- * and dtype; LSE (or NULL): fp32 [B, H_q, L], the natural logarithm of the sum of the
+ * and dtype, Q itself or no element of it; LSE (or NULL): fp32 [B, H_q, L], the natural logarithm of the sum of the
  * exponentials of the scaled scores.  A row that sees nothing gets O = 0 and LSE =
  * -infinity.  A NaN in a token reaches only rows that see it.  scale <= 0 selects
  * 1 / sqrt(d).  Scores and the softmax are fp32 for every dtype.

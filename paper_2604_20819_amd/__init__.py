@@ -406,18 +406,6 @@ def cqsa_backward(plan, Q, K, V, O, LSE, dO, dQ, dK, dV, scale=0.0, stream=None)
 
 
 # ------------------------------------------- rotary positions, 4-bit cache
-def as_cqsa_view(t):
-    """Describe a [B, L, H, d] torch tensor on a GPU, strided or not (no copy)."""
-    if t.dim() != 4:
-        raise ValueError("tensors must be [B, L, H, d]")
-    if not t.is_cuda:
-        raise ValueError("tensors must live on a GPU")
-    (B, L, H, d), (sb, sl, sh, sd) = t.shape, t.stride()
-    if sd != 1:
-        raise ValueError("the last dimension must be contiguous")
-    return cqsa_view(t.data_ptr(), _dtype_code(t), B, L, H, d, sb, sl, sh)
-
-
 # The calls of the operators: a step of decoding makes several of a few
 # microseconds each, so views are packed straight into cqsa_view's bytes (a
 # third of a ctypes structure's time).
@@ -639,10 +627,21 @@ def cqsa_cache_attend_workspace(cache, batch, Q):
     return _torch().empty(n.value, dtype=_torch().uint8, device=device) if n.value else None
 
 
+def _workspace_on(stream, cache, batch, Q):
+    """A workspace from torch's allocator for one call on `stream` (None: the current one)."""
+    if stream is None:
+        return cqsa_cache_attend_workspace(cache, batch, Q)
+    cuda = _torch().cuda
+    handle = getattr(stream, "value", stream) or 0
+    with cuda.stream(cuda.ExternalStream(handle, device=cache.device) if handle
+                     else cuda.default_stream(cache.device)):
+        return cqsa_cache_attend_workspace(cache, batch, Q)
+
+
 def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, workspace=None, stream=None):
     """Attention of the call's rows Q over their sequences' cached tokens into O
     and, if given, LSE (fp32 [B, Hq, L], packed [1, Hq, T]).  workspace=None
-    takes one from torch for this call."""
+    takes one from torch's allocator for this call and its stream."""
     device = _cache_device(cache, batch)
     vq, vo = _view(Q, device), _view(O, device)
     lse = None
@@ -653,9 +652,7 @@ def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, work
         lse = LSE.data_ptr()
     space, size = None, 0
     if workspace is None:
-        workspace = cqsa_cache_attend_workspace(cache, batch, Q)
-        if workspace is not None and stream is not None:
-            workspace.record_stream(_torch().cuda.ExternalStream(stream, device=device))
+        workspace = _workspace_on(stream, cache, batch, Q)
     if workspace is not None:
         if workspace.device != device or not workspace.is_contiguous():
             raise ValueError(f"the workspace must be a contiguous tensor on {device}")

@@ -103,6 +103,8 @@ cqsa_status move_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa
   if (K->H != c->H) return fail(CQSA_ERR_INVALID_ARG, what + "K's heads differ from the cache's");
   if ((st = check_rows(b, *K, what)) != CQSA_OK) return st;
   if (empty(*K) || b->B == 0) return CQSA_OK;
+  if (int64_t(b->B) * c->H > (int64_t(1) << 23))
+    return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences and heads than one launch takes");
   if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;
   CacheMoveArgs a{};
   a.c = args_of(c, b, *K);
@@ -132,8 +134,15 @@ cqsa_status check_attend(const cqsa_cache* c, const cqsa_cache_batch* b, const c
     return fail(CQSA_ERR_INVALID_ARG, what + "Q's heads must be a multiple of the cache's, at most 65536");
   if ((st = check_view(Q, "Q", c->d, false)) != CQSA_OK) return st;
   if ((st = check_rows(b, *Q, what)) != CQSA_OK) return st;
-  const int64_t n = b->q_start ? b->max_q : Q->L;
-  if (n * (Q->H / c->H) > (int64_t(1) << 30) || n * (Q->H / c->H) * c->H * b->B > (int64_t(1) << 30))
+  if (empty(*Q) || b->B == 0) return CQSA_OK;
+  // Work groups have 256 threads or more, and a launch fewer than 2^32 of them.
+  const int64_t rows = int64_t(b->q_start ? b->max_q : Q->L) * (Q->H / c->H);
+  const int64_t heads = int64_t(b->B) * c->H;
+  if (rows > (int64_t(1) << 30) || heads > (int64_t(1) << 23) ||
+      heads * ((rows + 15) / 16) > (int64_t(1) << 27))
+    return fail(CQSA_ERR_UNSUPPORTED, what + "more rows than one launch takes");
+  const AttendPlan p = attend_plan(c, b, *Q);
+  if (heads * p.row_tiles * p.splits > (int64_t(1) << 23))
     return fail(CQSA_ERR_UNSUPPORTED, what + "more rows than one launch takes");
   return CQSA_OK;
 }

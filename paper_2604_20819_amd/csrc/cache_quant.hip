@@ -256,8 +256,7 @@ hipError_t launch_move(cqsa_dtype dt, const CacheMoveArgs& a, hipStream_t s) {
   int64_t per = n == 1 ? 1 : (n + 30) / 32 + 1;
   // a work group for each (a prompt of 262144 tokens: 270 us; 16 times fewer groups, 287)
   const int64_t most = (int64_t(1) << 23) / (int64_t(a.c.B) * groups);
-  if (per > most) per = most;
-  if (per < 1) per = 1;
+  if (per > most) per = most;  // B and the heads are at most 2^23 together
   const dim3 grid(unsigned(per * a.c.B * groups));
   if (dt == CQSA_BF16)
     launch_rows<__bf16, WRITE>(a, grid, groups, int(per), s);

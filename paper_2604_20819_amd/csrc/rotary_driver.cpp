@@ -140,6 +140,8 @@ cqsa_status rotary_impl(const cqsa_rotary_s* p, const int32_t* pos, const cqsa_v
     if (!same && views_meet(x[k], y[k]))
       return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: y overlaps x without being x");
   }
+  if (heads > (1 << 20))
+    return fail(CQSA_ERR_UNSUPPORTED, "cqsa_rotary: more than 2^20 heads");
   const int64_t rows = x[0].B * x[0].L;
   if (rows == 0 || heads == 0) return CQSA_OK;
   if (!pos) return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: pos is NULL");
@@ -166,9 +168,7 @@ cqsa_status rotary_impl(const cqsa_rotary_s* p, const int32_t* pos, const cqsa_v
   a.parts = uint32_t(std::max<int64_t>((a.H + batch - 1) / batch,
                                        std::min<int64_t>(a.H, ((1 << 18) + per - 1) / per)));
   const int64_t per_row = int64_t(a.units) * a.parts;
-  const int64_t slab = std::max<int64_t>(1, (int64_t(1) << 30) / per_row);
-  if (per_row > (int64_t(1) << 30))
-    return fail(CQSA_ERR_UNSUPPORTED, "cqsa_rotary: more heads than one launch takes");
+  const int64_t slab = (int64_t(1) << 30) / per_row;  // rows of a launch; per_row <= 2^24
   for (int64_t r = 0; r < rows; r += slab) {
     a.row0 = r;
     a.n = uint32_t(std::min(slab, rows - r) * per_row);

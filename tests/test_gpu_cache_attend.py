@@ -46,11 +46,17 @@ def held(dtype, O, LSE, ref, tokens):
     assert (off <= bound).all(), (off - bound).max()
 
 
-def run(case, q, lens=None, causal=True, scale=0.0, cache=None, dtype="bf16", check=True, **kw):
+# The launch goes by the lengths' bound, so a bound far above the lengths takes short
+# sequences through the kernels and splits that long ones get: one group of 16 rows a
+# wave, two, the kernel for many rows (more than 64).
+BOUNDS = {"few": 0, "two": 1 << 17, "many": 1 << 22}
+
+
+def run(case, q, lens=None, causal=True, scale=0.0, cache=None, dtype="bf16", check=True, kind="few", **kw):
     """The call on uniform rows q [B, n, Hq, d]; checked against the oracle."""
     B, n, Hq, d = q.shape
     cache = cache or case.cache()
-    batch = case.batch(lens=lens, **kw)
+    batch = bounded(case, kind, lens=lens, **kw)
     O = torch.full_like(q, 9.0, device="cuda")
     LSE = torch.full((B, Hq, n), 9.0, device="cuda")
     cq.cqsa_cache_attend(cache, batch, q.cuda(), O, LSE, causal=causal, scale=scale)
@@ -61,6 +67,17 @@ def run(case, q, lens=None, causal=True, scale=0.0, cache=None, dtype="bf16", ch
             ref = reference(case, synth.as_f64(q)[b], b, length, causal, scale)
             held(dtype, O[b].cpu().double().numpy(), LSE[b].t().cpu().double().numpy(), ref, max(length, 1))
     return O, LSE
+
+
+def bounded(case, kind, lens=None, **kw):
+    """The batch with a wide table where the bound needs one."""
+    if not BOUNDS[kind]:
+        return case.batch(lens=lens, **kw)
+    wide = np.full((case.table.shape[0], BOUNDS[kind] // case.page), -1, np.int32)
+    wide[:, :case.table.shape[1]] = case.table
+    return cq.CacheBatch(torch.from_numpy(wide).cuda(),
+                         torch.tensor(case.lens if lens is None else lens, dtype=torch.int32, device="cuda"),
+                         **{"max_len": BOUNDS[kind], **kw})
 
 
 def reference(case, q, b, length, causal, scale=0.0):
@@ -108,6 +125,57 @@ def test_types_and_rows(dtype, d, G, n):
     run(case, normal(case.g, (2, n, G, d), dtype), dtype=dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_many_rows(dtype, d):
+    """The kernel for many rows: rows that end inside a wave and a work group, a sequence of fewer
+    tokens than rows, one of none."""
+    need_gpu()
+    lens, n, G = (307, 70, 0), 97, 3
+    case = Case(d + 7, lens, 1, d, 32)
+    case.fill_tokens()
+    say("attend many", dtype, d)
+    q = normal(case.g, (3, n, G, d), dtype)
+    run(case, q, dtype=dtype, kind="many")
+    run(case, q[:, :25].contiguous(), dtype=dtype, kind="many", causal=False)
+
+
+@pytest.mark.parametrize("dtype,d,kind,n", [("bf16", 128, "two", 5), ("f16", 96, "two", 9), ("bf16", 64, "two", 15),
+                                            ("f16", 32, "two", 5), ("bf16", 128, "many", 40), ("f16", 64, "many", 70)])
+def test_split_rows(dtype, d, kind, n):
+    """Two groups of 16 rows a wave, and many rows, over contexts that are split."""
+    need_gpu()
+    lens, G = (3001, 64, 1499), 4
+    case = Case(d + n, lens, 2, d, 64)
+    case.fill_tokens()
+    say("attend split", dtype, d, kind, n)
+    run(case, normal(case.g, (3, n, 2 * G, d), dtype), dtype=dtype, kind=kind)
+
+
+def test_kinds_take_the_launches_that_the_tests_mean():
+    """By the workspace: a split call has one."""
+    need_gpu()
+    case = Case(3, (300, 70), 1, 64, 32)
+    case.fill_tokens()
+    for kind in BOUNDS:
+        q = torch.zeros((2, 70, 2, 64), dtype=torch.bfloat16, device="cuda")
+        space = cq.cqsa_cache_attend_workspace(case.cache(), bounded(case, kind), q)
+        assert (space is None) == (kind == "few")
+
+
+@pytest.mark.parametrize("n,kind", [(1, "few"), (3, "two"), (30, "many")])
+def test_result_over_the_queries(n, kind):
+    """O may be Q."""
+    need_gpu()
+    case = Case(67, (300, 65), 2, 64, 64)
+    case.fill_tokens()
+    q = normal(case.g, (2, n, 8, 64), "bf16")
+    O, _ = run(case, q, kind=kind)
+    x = q.cuda()
+    cq.cqsa_cache_attend(case.cache(), bounded(case, kind), x, x)
+    assert torch.equal(x, O)
+
+
 @pytest.mark.parametrize("lens,n,G,B_pad", [((20011,), 1, 4, 0), ((9000, 17, 4097), 3, 2, 0),
                                             ((6000,), 40, 1, 30), ((2500, 5000), 1, 16, 60)])
 def test_long_contexts(lens, n, G, B_pad):
@@ -121,16 +189,19 @@ def test_long_contexts(lens, n, G, B_pad):
     run(case, normal(case.g, (len(lens), n, G, d), "bf16"))
 
 
-def test_packed_rows():
+@pytest.mark.parametrize("kind,G,dtype", [("few", 3, "bf16"), ("few", 3, "f32"), ("two", 1, "f16"), ("many", 3, "bf16")])
+def test_packed_rows(kind, G, dtype):
     """Ragged rows; rows of no sequence stay as they were, LSE's too."""
     need_gpu()
     lens, new, first = (70, 40, 333, 3, 128), (65, 0, 1, 9, 128), 3
-    H, G, d = 2, 3, 96
+    H, d = 2, 96
+    if kind == "two":  # as many rows as that takes
+        lens, new = (70, 40, 333, 3, 60), (55, 0, 1, 9, 60)
     case = Case(17, lens, H, d, 32)
     case.fill_tokens()
     T = first + sum(new) + 4
-    q = normal(case.g, (1, T, H * G, d), "bf16")
-    batch = case.batch(q_start=starts(new, first), max_q=128)
+    q = normal(case.g, (1, T, H * G, d), dtype)
+    batch = bounded(case, kind, q_start=starts(new, first), max_q=max(new))
     O = torch.full_like(q, 9.0, device="cuda")
     LSE = torch.full((1, H * G, T), 9.0, device="cuda")
     cq.cqsa_cache_attend(case.cache(), batch, q.cuda(), O, LSE)
@@ -138,12 +209,13 @@ def test_packed_rows():
     o, l = O[0].cpu().double().numpy(), LSE[0].t().cpu().double().numpy()
     for b, n in enumerate(lens):
         r = slice(off[b], off[b + 1])
-        held("bf16", o[r], l[r], reference(case, synth.as_f64(q)[0, r], b, n, True), n)
+        held(dtype, o[r], l[r], reference(case, synth.as_f64(q)[0, r], b, n, True), n)
     for x in (o, l):
         assert (x[:first] == 9).all() and (x[off[-1]:] == 9).all()
 
 
-def test_given_up_pages_and_bad_entries():
+@pytest.mark.parametrize("kind,rows", [("few", (1, 50)), ("two", (17,)), ("many", (33, 150))])
+def test_given_up_pages_and_bad_entries(kind, rows):
     """Entries outside the pool hold no tokens; a sequence of only such ones is empty."""
     need_gpu()
     lens, d = (200, 130, 64, 70), 64
@@ -153,8 +225,8 @@ def test_given_up_pages_and_bad_entries():
     case.table[0, 4] = case.n_pages + 7
     case.table[1, 4] = -2 ** 31
     case.table[2, :] = 2 ** 31 - 1
-    for n in (1, 50):
-        run(case, normal(case.g, (4, n, 2, d), "bf16"))
+    for n in rows:
+        run(case, normal(case.g, (4, n, 2, d), "bf16"), kind=kind)
 
 
 def test_lengths_out_of_range():
@@ -168,8 +240,9 @@ def test_lengths_out_of_range():
         held("bf16", O[b].cpu().double().numpy(), LSE[b].t().cpu().double().numpy(), ref, max(n, 1))
 
 
-@pytest.mark.parametrize("n,G", [(1, 1), (6, 1), (70, 2)])
-def test_not_a_number_reaches_only_rows_that_see_it(n, G):
+@pytest.mark.parametrize("n,G,kind", [(1, 1, "few"), (6, 1, "few"), (70, 2, "few"), (20, 1, "two"),
+                                      (70, 2, "two"), (70, 2, "many"), (290, 1, "many"), (199, 1, "many")])
+def test_not_a_number_reaches_only_rows_that_see_it(n, G, kind):
     """A NaN or an infinity in a key makes the rows that see it NaN; in a value, their 32 channels;
     other rows keep their bits."""
     need_gpu()
@@ -178,12 +251,12 @@ def test_not_a_number_reaches_only_rows_that_see_it(n, G):
         case = Case(31, (200,), H, d, 64)
         rows = case.fill_tokens()
         q = normal(case.g, (1, n, G, d), "bf16")
-        O, LSE = run(case, q)
+        O, LSE = run(case, q, kind=kind)
         k, v = (x.copy() for x in rows[0])
         (k if what == "k" else v)[at, 0, 35] = np.nan if at == 150 else np.inf
         p, t = case.slots(0, 0, 200)
         o4.write(case.data, 64, k, v, p, t)
-        O2, LSE2 = run(case, q, check=False)
+        O2, LSE2 = run(case, q, check=False, kind=kind)
         for i in range(n):
             sees = at <= 200 - n + i
             same = torch.equal(O2[0, i], O[0, i]) and torch.equal(LSE2[0, :, i], LSE[0, :, i])
@@ -196,17 +269,18 @@ def test_not_a_number_reaches_only_rows_that_see_it(n, G):
                 assert torch.equal(LSE2[0, :, i], LSE[0, :, i])
 
 
+@pytest.mark.parametrize("kind", ["few", "two", "many"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_query_that_is_not_finite(bad):
+def test_query_that_is_not_finite(bad, kind):
     """Its own row is NaN, the other rows keep their bits."""
     need_gpu()
     case = Case(37, (90,), 1, 64, 32)
     case.fill_tokens()
-    q = normal(case.g, (1, 20, 3, 64), "bf16")
-    O, LSE = run(case, q)
+    q = normal(case.g, (1, 23, 3, 64), "bf16")
+    O, LSE = run(case, q, kind=kind)
     q2 = q.clone()
     q2[0, 7, 1, 50] = bad
-    O2, LSE2 = run(case, q2, check=False)
+    O2, LSE2 = run(case, q2, check=False, kind=kind)
     assert O2[0, 7, 1].isnan().all() and LSE2[0, 1, 7].isnan()
     O2[0, 7, 1], LSE2[0, 1, 7] = O[0, 7, 1], LSE[0, 1, 7]
     assert torch.equal(O2, O) and torch.equal(LSE2, LSE)
@@ -247,15 +321,17 @@ def test_strided_and_without_lse():
     assert torch.equal(view, O) and (out[..., :d] == 9).all()
 
 
-@pytest.mark.parametrize("n,lens", [(1, (5000, 30)), (64, (700, 64))])
-def test_captured_on_streams_and_repeated(n, lens):
+@pytest.mark.parametrize("n,lens,kind", [(1, (5000, 30), "few"), (64, (700, 64), "few"), (8, (700, 64), "two"),
+                                         (40, (1700, 64), "many")])
+def test_captured_on_streams_and_repeated(n, lens, kind):
     """Replays follow the lengths, tables and rows on the device; the same call gives the same
     bits on any stream, with a workspace of any contents."""
     need_gpu()
     H, G, d = 1, 4, 64
     case = Case(53, lens, H, d, 64)
     case.fill_tokens()
-    cache, batch = case.cache(), case.batch(max_len=case.table.shape[1] * 64)
+    cache = case.cache()
+    batch = bounded(case, kind, max_len=BOUNDS[kind] or case.table.shape[1] * 64)
     q = normal(case.g, (2, n, G, d), "bf16").cuda()
     O, LSE = torch.empty_like(q), torch.empty((2, G, n), device="cuda")
     space = cq.cqsa_cache_attend_workspace(cache, batch, q)

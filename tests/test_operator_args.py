@@ -193,6 +193,41 @@ def test_more_of_attend_refused():
     assert n.value == 0
 
 
+def test_calls_too_large_for_a_launch():
+    lib, far = cq.lib(), dict(data=PTR + (1 << 40))
+    n = ctypes.c_uint64()
+
+    def unsupported(status):
+        assert status == -2 and "launch" in lib.cqsa_last_error().decode()
+
+    B = 1 << 20
+    many = view(B=B, L=1, H=16, stride_b=0)
+    c, b = cache(H=16), batch(B=B, max_pages=5, pages_stride=5)
+    for f in (lib.cqsa_cache_write, lib.cqsa_cache_read):
+        out = view(B=B, L=1, H=16, stride_b=16 * 64, **far)
+        unsupported(f(c, b, out, out, None))
+    unsupported(lib.cqsa_cache_attend_workspace(c, b, many, n))
+    long = view(B=1, L=1 << 30, H=4, stride_b=0, stride_l=0)
+    unsupported(lib.cqsa_cache_attend_workspace(cache(H=1), batch(B=1), long, n))
+    unsupported(lib.cqsa_cache_attend_workspace(cache(), batch(B=8), view(B=8, L=1 << 29, stride_b=0, stride_l=0), n))
+    keep = cq.cqsa_rotary_plan(64)
+    wide = view(B=1, L=1, H=(1 << 20) + 1)
+    assert lib.cqsa_rotary(keep.handle, PTR, wide, view(B=1, L=1, H=(1 << 20) + 1, **far), 1, 0, None) == -2
+
+
+def test_workspace_by_the_sizes_alone():
+    """None for short contexts; splits x rows x (d + 4) floats for long ones, also where Q's data is not there."""
+    lib, n = cq.lib(), ctypes.c_uint64(7)
+    q = view(L=1)
+    assert lib.cqsa_cache_attend_workspace(cache(), batch(), q, n) == 0 and n.value == 0
+    b = batch(max_pages=1 << 14, pages_stride=1 << 14, max_len=1 << 20)
+    assert lib.cqsa_cache_attend_workspace(cache(), b, q, n) == 0 and n.value > 0
+    assert n.value % (2 * 4 * (64 + 4) * 4) == 0
+    # too small, missing and misaligned ones are refused
+    for space, size, text in ((None, 0, "workspace"), (PTR, n.value - 1, "workspace"), (PTR + 8, n.value, "16-byte")):
+        refused(lib.cqsa_cache_attend(cache(), b, q, view(L=1, data=PTR + (1 << 32)), None, 1, 0.0, space, size, None), text)
+
+
 def test_write_and_read_views_refused():
     lib = cq.lib()
     for f in (lib.cqsa_cache_write, lib.cqsa_cache_read):
