@@ -58,6 +58,7 @@ struct AttendArgs {
 // How a call's rows and tokens are spread over work groups; by its sizes alone.
 struct AttendPlan {
   int row_groups;  // of 16 rows, for each wave; 0: cache_attend_many
+  int waves;       // of a work group for few rows: 4, or as many as fill a CU
   int row_tiles;   // work groups over a sequence's and head's rows
   int splits;      // work groups over a sequence's tokens
   int min_chunk;   // tiles that a split takes at least

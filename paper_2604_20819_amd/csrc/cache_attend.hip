@@ -1,10 +1,16 @@
 // Attention over the 4-bit cache for few rows a sequence (gfx950): decoding.
 //
 // A key head's G query heads of a sequence's n tokens are n G rows of one matrix
-// product with its keys, 16 NQ of them a work group.  The four waves of a work
-// group take 32-token tiles in turn and keep a running maximum, sum and
-// unnormalised result each, which are joined at the end through LDS; a long
-// sequence is split over `splits` work groups, joined by a second kernel.
+// product with its keys, 16 NQ of them a work group.  The W waves of a work group
+// take 32-token tiles in turn and keep a running maximum, sum and unnormalised
+// result each, which are joined at the end through LDS; a long sequence is split
+// over `splits` work groups, joined by a second kernel.
+//
+// What bounds it: the cache's bytes where they are many (one sequence of 2^20
+// tokens, 8 heads, d = 128: 1.14 GB in 207 us, 5.5 TB/s; a copy reaches 4.7),
+// some 7 us of start, dependent loads and end where they are few (500 tokens 7.5
+// us).  A tile of d = 128 is 300 vector instructions a wave, half of them the
+// decoding: about half of the SIMDs' time in the first of these calls.
 //
 // Per tile, lane (q, c) = (lane / 16, lane % 16) holds keys 16 t + c (t = 0, 1):
 // where d is a multiple of 128 the blocks 4 j + q, 16 bytes of codes each (the
@@ -20,8 +26,6 @@ namespace cqsa {
 
 namespace {
 
-constexpr int kWaves = 4;
-
 // Waves a SIMD is to hold (and work groups a CU): as many as the registers
 // allow without spilling.  `parts` of the queries, blocks of 32 channels, groups
 // of 16 rows.
@@ -34,16 +38,16 @@ constexpr int few_waves(int parts, int db, int nq) {
 
 }  // namespace
 
-template <typename T, int DB, int NQ>
-__global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB, NQ)))
+template <typename T, int DB, int NQ, int W>
+__global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)))
     cache_attend_few(const AttendArgs a, int row_tiles, int splits, int min_chunk) {
   constexpr bool WIDE = DB % 4 == 0;  // whole blocks a lane
   constexpr int D = 32 * DB, QP = RowType<T>::kQuery, WP = NQ == 1 ? RowType<T>::kWeightFew : RowType<T>::kWeight;
   constexpr int ROWS = 16 * NQ, QSTRIDE = 2 * D + 16;  // 16: rows on different banks
   constexpr int OSTRIDE = D + 4;
-  constexpr int QBYTES = QP * ROWS * QSTRIDE, OBYTES = kWaves * 16 * OSTRIDE * 4;
+  constexpr int QBYTES = QP * ROWS * QSTRIDE, SLOTS = W > 4 ? W / 2 : W, OBYTES = SLOTS * 16 * OSTRIDE * 4;
   __shared__ __attribute__((aligned(16))) char lds[QBYTES > OBYTES ? QBYTES : OBYTES];
-  __shared__ float stat[kWaves][ROWS][2];
+  __shared__ float stat[W][ROWS][2];
 
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
@@ -77,7 +81,7 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
 
   // pages of this wave's next 64 tiles, one a lane
   auto window = [&](int t) {
-    const int u = t + kWaves * lane;
+    const int u = t + W * lane;
     return u < t1 ? int32_t(page_of(c, b, u)) : -1;
   };
   // What a wave holds of a tile: the keys are used first, so the next tile's are
@@ -134,7 +138,7 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
   }
 
   // queries, split into operands
-  for (int u = tid; u < ROWS * 4 * DB; u += 64 * kWaves) {
+  for (int u = tid; u < ROWS * 4 * DB; u += 64 * W) {
     const int r = u / (4 * DB), e = 8 * (u % (4 * DB));
     float v[8];
     if (r0 + r < rows) {
@@ -284,13 +288,13 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
     }
   };
 
-  for (int t = t0 + wave; t < t1; t += kWaves) {
-    const int32_t next = next_page(t + kWaves);
+  for (int t = t0 + wave; t < t1; t += W) {
+    const int32_t next = next_page(t + W);
     const bool here = page >= 0;
     if (here) score();
-    if (next >= 0) load_keys(t + kWaves, next);
+    if (next >= 0) load_keys(t + W, next);
     if (here) weigh(t);
-    if (next >= 0) load_values(t + kWaves, next);
+    if (next >= 0) load_values(t + W, next);
     page = next;
   }
 
@@ -308,32 +312,57 @@ __global__ void __launch_bounds__(64 * kWaves, (few_waves(RowType<T>::kQuery, DB
   for (int n = 0; n < NQ; ++n) {
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w][16 * n + col][0]);
-    const float f = m[n] == -INFINITY ? 0.f : fast_exp2(m[n] - top);
-    float* dst = (float*)lds + (wave * 16 + col) * OSTRIDE + 8 * quarter;
+    for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w][16 * n + col][0]);
+    // m is -inf where every score was (or none was seen): NaN that came by a
+    // value or a score stays
+    const float f = m[n] == -INFINITY ? 1.f : fast_exp2(m[n] - top);
 #pragma unroll
-    for (int k = 0; k < DB; ++k) {
-      const f32x4 e = o[n][k][0], q = o[n][k][1];
-      // m is -inf where every score was (or none was seen): NaN that came by a
-      // value or a score stays
-      const float g = m[n] == -INFINITY ? 1.f : f;
-      *(f32x4*)(dst + 32 * k) = f32x4{e[0] * g, q[0] * g, e[1] * g, q[1] * g};
-      *(f32x4*)(dst + 32 * k + 4) = f32x4{e[2] * g, q[2] * g, e[3] * g, q[3] * g};
+    for (int k = 0; k < DB; ++k) o[n][k][0] *= f, o[n][k][1] *= f;
+    auto slot = [&](int w) { return (float*)lds + (w * 16 + col) * OSTRIDE + 8 * quarter; };
+    auto put = [&](float* dst) {
+#pragma unroll
+      for (int k = 0; k < DB; ++k) {
+        const f32x4 e = o[n][k][0], q = o[n][k][1];
+        *(f32x4*)(dst + 32 * k) = f32x4{e[0], q[0], e[1], q[1]};
+        *(f32x4*)(dst + 32 * k + 4) = f32x4{e[2], q[2], e[3], q[3]};
+      }
+    };
+    // more than four waves: half of them add the other half's, until four or
+    // three are left
+    int live = W;
+#pragma unroll
+    while (live > 4) {
+      live /= 2;
+      if (wave >= live && wave < 2 * live) put(slot(wave - live));
+      __syncthreads();
+      if (wave < live) {
+        const float* src = slot(wave);
+#pragma unroll
+        for (int k = 0; k < DB; ++k) {
+          const f32x4 x = *(const f32x4*)(src + 32 * k), y = *(const f32x4*)(src + 32 * k + 4);
+          o[n][k][0] += f32x4{x[0], x[2], y[0], y[2]};
+          o[n][k][1] += f32x4{x[1], x[3], y[1], y[3]};
+        }
+      }
+      __syncthreads();
     }
+    if (wave < live) put(slot(wave));
     __syncthreads();
-    for (int u = tid; u < 16 * 4 * DB; u += 64 * kWaves) {
+    for (int u = tid; u < 16 * 4 * DB; u += 64 * W) {
       const int rr = u / (4 * DB), ch = 8 * (u % (4 * DB)), r = r0 + 16 * n + rr;
       if (r < rows) {
         float mt = -INFINITY, lt = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) mt = fmaxf(mt, stat[w][16 * n + rr][0]);
+        for (int w = 0; w < W; ++w) mt = fmaxf(mt, stat[w][16 * n + rr][0]);
         float acc[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
           const float mw = stat[w][16 * n + rr][0];
           lt += stat[w][16 * n + rr][1] * (mw == -INFINITY ? 1.f : fast_exp2(mw - mt));
+        }
+        for (int w = 0; w < live; ++w) {
           const float* src = (const float*)lds + (w * 16 + rr) * OSTRIDE + ch;
 #pragma unroll
           for (int e = 0; e < 8; ++e) acc[e] += src[e];
@@ -425,15 +454,26 @@ __global__ void __launch_bounds__(256) cache_attend_join(const AttendArgs a, int
 
 namespace {
 
+template <typename T, int NQ, int DB>
+void launch_waves(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
+  const unsigned grid = unsigned(int64_t(a.c.B) * a.c.H * p.row_tiles * p.splits);
+  constexpr int W = 4 * few_waves(RowType<T>::kQuery, DB, 1);
+  if constexpr (NQ == 1 && W > 4)
+    if (p.waves > 4) {
+      hipLaunchKernelGGL((cache_attend_few<T, DB, 1, W>), dim3(grid), dim3(64 * W), 0, s, a, p.row_tiles, p.splits,
+                         p.min_chunk);
+      return;
+    }
+  hipLaunchKernelGGL((cache_attend_few<T, DB, NQ, 4>), dim3(grid), dim3(256), 0, s, a, p.row_tiles, p.splits,
+                     p.min_chunk);
+}
+
 template <typename T, int NQ>
 hipError_t launch_few(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  const dim3 grid(unsigned(int64_t(a.c.B) * a.c.H * p.row_tiles * p.splits)), block(64 * kWaves);
   switch (a.c.d) {
-#define CQSA_FEW(DB)                                                                             \
-  case 32 * DB:                                                                                  \
-    if constexpr (NQ == 1 || DB <= 4)                                                            \
-      hipLaunchKernelGGL((cache_attend_few<T, DB, NQ>), grid, block, 0, s, a, p.row_tiles, p.splits, \
-                       p.min_chunk); \
+#define CQSA_FEW(DB)                                              \
+  case 32 * DB:                                                   \
+    if constexpr (NQ == 1 || DB <= 4) launch_waves<T, NQ, DB>(a, p, s); \
     break;
     CQSA_FEW(1)
     CQSA_FEW(2)
@@ -531,6 +571,16 @@ AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa
   const int64_t least = 2 * groups >= slots ? 96 : (B == 1 ? 8 : std::max<int64_t>(16, std::min<int64_t>(24, once)));
   int64_t chunk = std::max<int64_t>(least, B > 1 ? (once + 3) / 4 : once);
   if (tiles <= 16) chunk = 16;
+  // Work groups that fill a CU, where one for each sequence, head and rows keeps
+  // more than half of the CUs busy, or where a part would be a wave's few tiles:
+  // no join (32 sequences of up to 2500 tokens 18.6 us, split 20.6, 16 of them
+  // 16.9 and 16.0; 4 of up to 700 9.6 and 11.0, of 1500 12.7 and 11.2).
+  const int wide = p.row_groups == 1 ? 4 * few_waves(parts, d / 32, 1) : 4;
+  p.waves = 4;
+  if (wide > 4 && groups <= 256 && (groups > 128 ? tiles <= 128 : (wide > 8 && tiles <= 24))) {
+    p.waves = wide;
+    chunk = tiles + 1;
+  }
   p.splits = int(std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, (tiles + chunk - 1) / chunk)));
   p.min_chunk = int(std::min<int64_t>(chunk, 1 << 30));
   return p;

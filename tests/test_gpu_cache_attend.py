@@ -177,7 +177,8 @@ def test_result_over_the_queries(n, kind):
 
 
 @pytest.mark.parametrize("lens,n,G,B_pad", [((20011,), 1, 4, 0), ((9000, 17, 4097), 3, 2, 0),
-                                            ((6000,), 40, 1, 30), ((2500, 5000), 1, 16, 60)])
+                                            ((6000,), 40, 1, 30), ((2500, 5000), 1, 16, 60),
+                                            ((2000, 40), 1, 16, 150), ((900, 333), 2, 3, 0)])
 def test_long_contexts(lens, n, G, B_pad):
     """Contexts that are split over work groups, alone and beside many short sequences."""
     need_gpu()
