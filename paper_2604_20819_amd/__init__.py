@@ -7,7 +7,8 @@ not been built (``python -m paper_2604_20819_amd.build``); there is no CPU or
 eager fallback.
 
 Names follow include/cqsa.h: ``cqsa_plan``, ``cqsa_forward``,
-``cqsa_backward``, ``cqsa_set_timing``, ``cqsa_last_stats`` ...
+``cqsa_backward``, ``cqsa_set_timing``, ``cqsa_last_stats``,
+``cqsa_rotary``, ``cqsa_cache_write``, ``cqsa_cache_attend`` ...
 """
 import ctypes
 import os

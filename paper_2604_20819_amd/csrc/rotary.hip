@@ -14,39 +14,30 @@ namespace cqsa {
 
 namespace {
 
-// Two runs of 8 elements.  A run of fp32 is two vectors, `far` elements apart,
-// so that every load and store of neighbouring lanes covers whole lines.
+// What a thread holds of a head: two vectors of 16 bytes.
 template <typename T>
-struct Vec16 {
-  static constexpr int N = 16 / sizeof(T), V = 8 / N;  // of a 16-byte vector, vectors of a run
+struct Pair16 {
+  static constexpr int N = 16 / sizeof(T);
   typedef __attribute__((__vector_size__(16))) T vec;
-  vec x[2 * V];
-  __device__ __forceinline__ void load(const T* p, const T* q, uint32_t far) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = *(const vec*)(p + i * far), x[V + i] = *(const vec*)(q + i * far);
-  }
+  vec x[2];
+  __device__ __forceinline__ void load(const T* p, const T* q) { x[0] = *(const vec*)p, x[1] = *(const vec*)q; }
   template <bool LINES>
-  __device__ __forceinline__ void store(T* p, T* q, uint32_t far) const {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      vec* const a = (vec*)(p + i * far);
-      vec* const b = (vec*)(q + i * far);
-      if constexpr (LINES) {
-        __builtin_nontemporal_store(x[i], a);
-        __builtin_nontemporal_store(x[V + i], b);
-      } else {
-        *a = x[i];
-        *b = x[V + i];
-      }
+  __device__ __forceinline__ void store(T* p, T* q) const {
+    if constexpr (LINES) {
+      __builtin_nontemporal_store(x[0], (vec*)p);
+      __builtin_nontemporal_store(x[1], (vec*)q);
+    } else {
+      *(vec*)p = x[0];
+      *(vec*)q = x[1];
     }
   }
   __device__ __forceinline__ void get(float* f) const {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = float(x[i / N][i % N]);
+    for (int i = 0; i < 2 * N; ++i) f[i] = float(x[i / N][i % N]);
   }
   __device__ __forceinline__ void set(const float* f) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i / N][i % N] = T(f[i]);
+    for (int i = 0; i < 2 * N; ++i) x[i / N][i % N] = T(f[i]);
   }
 };
 
@@ -66,41 +57,40 @@ __device__ __forceinline__ void sin_cos_turns(uint32_t v, float* s, float* c) {
 
 }  // namespace
 
-// One thread turns a chunk of 8 pairs of the heads part, part + parts, ... of
-// one row; the chunk's angles, some 300 instructions, are computed once for
-// all of them.  rotary_batch heads are read before the first of them is written:
-// 8 of 16 bits, 4 of 32 (32768 rows of 32 heads, bf16, d = 128: 83 us with 8, 97
-// with 4; 131072 of 16, fp32, d = 64: 222 and 216).  Where 8 lanes side by side
-// write a line of 128 bytes at once, they write it past the caches, which it
-// would only pass through (the same rows: 97 and 149 us); written in halves, it
-// is better gathered there (fp32, d = 64: 216 and 197).
+// One thread turns a chunk of N pairs, N the elements of 16 bytes, of the heads
+// part, part + parts, ... of one row; the chunk's angles, some 40 instructions
+// each, are computed once for all of them.  A chunk is two vectors, each beside
+// its neighbours' in every load and store: N pairs across them, or N / 2 within
+// each.  kRotaryBatch heads are read before the first of them is written (32768
+// rows of 32 heads, bf16, d = 128: 83 us with 8, 97 with 4).  Where 8 lanes side
+// by side write a line of 128 bytes at once, they write it past the caches,
+// which it would only pass through (the same rows: 97 and 149 us); written in
+// halves, it is better gathered there.
 template <typename T, bool ADJACENT, bool LINES>
 __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
-  constexpr int BATCH = rotary_batch(sizeof(T));
+  constexpr int BATCH = kRotaryBatch, N = Pair16<T>::N;
   const uint32_t i = blockIdx.x * 256 + threadIdx.x;
   if (i >= a.n) return;
   const uint32_t u = i % a.units, part = i / a.units % a.parts;
   const int64_t row = a.row0 + i / (a.units * a.parts);
   const int64_t b = row / a.L, l = row % a.L;
   const bool turned = u < a.chunks;
-  float sn[8], cs[8];
-  // The chunk's two runs of 8 elements: 8 pairs across the runs, or 4 within each.
-  constexpr uint32_t N = Vec16<T>::N;
-  const uint32_t e0 = turned ? N * u : 16 * u, e1 = e0 + (turned ? a.pairs : 8);
-  const uint32_t far = turned ? a.pairs / 2 : N;
+  float sn[N], cs[N];
+  // the first vector's elements, and the second's: of the pairs, or of the rest
+  // in its two halves
+  const uint32_t e0 = N * u + (turned ? 0 : a.pairs);
+  const uint32_t e1 = e0 + (turned ? a.pairs : N * (a.units - a.chunks));
   if (turned) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // of the run's elements e (and of those in the other run that are its like)
-      const uint32_t k = ADJACENT ? 2 * (j % 4) : j, e = N * u + k / N * far + k % N;
-      const uint32_t pair = ADJACENT ? (j / 4 * a.pairs + e) / 2 : e;
+    for (int j = 0; j < N; ++j) {
+      const uint32_t pair = ADJACENT ? (j < N / 2 ? e0 / 2 + j : e1 / 2 + j - N / 2) : e0 + j;
       const int64_t p = a.pos[a.tab.axis[pair] * a.rows + row];
       sin_cos_turns(uint32_t((uint64_t(p) * a.tab.turn[pair]) >> 32), &sn[j], &cs[j]);
       if (a.inverse) sn[j] = -sn[j];
     }
   }
   for (uint32_t h0 = part; h0 < a.H; h0 += BATCH * a.parts) {
-    Vec16<T> v[BATCH];
+    Pair16<T> v[BATCH];
     T* y[BATCH];
 #pragma unroll
     for (int k = 0; k < BATCH; ++k) {
@@ -110,24 +100,24 @@ __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
         const int64_t h = hv - (hv >= a.H0 ? a.H0 : 0);
         const T* x = (const T*)t.x + b * t.x_b + l * t.x_l + h * t.x_h;
         y[k] = (T*)t.y + b * t.y_b + l * t.y_l + h * t.y_h;
-        v[k].load(x + e0, x + e1, far);
+        v[k].load(x + e0, x + e1);
       }
     }
 #pragma unroll
     for (int k = 0; k < BATCH; ++k)
       if (h0 + k * a.parts < a.H) {
         if (turned) {
-          float x[16], w[16];
+          float x[2 * N], w[2 * N];
           v[k].get(x);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int p = ADJACENT ? 2 * j : j, q = ADJACENT ? 2 * j + 1 : j + 8;
+          for (int j = 0; j < N; ++j) {
+            const int p = ADJACENT ? 2 * j : j, q = ADJACENT ? 2 * j + 1 : j + N;
             w[p] = x[p] * cs[j] - x[q] * sn[j];
             w[q] = x[q] * cs[j] + x[p] * sn[j];
           }
           v[k].set(w);
         }
-        v[k].template store<LINES>(y[k] + e0, y[k] + e1, far);
+        v[k].template store<LINES>(y[k] + e0, y[k] + e1);
       }
   }
 }

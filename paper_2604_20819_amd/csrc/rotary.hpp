@@ -29,16 +29,15 @@ struct RotaryArgs {
   uint32_t n;          // threads of this launch with work
   uint32_t L;
   uint32_t H0, H;      // heads of the first tensor, of both
-  uint32_t chunks;     // chunks of 8 pairs (16 elements) of a head that are turned
-  uint32_t units;      // chunks and, out of place, the 16-element pieces that are copied
+  uint32_t chunks;     // threads' chunks (two vectors of 16 bytes) of a head that are turned
+  uint32_t units;      // and, out of place, those that are copied
   uint32_t parts;      // threads that share a row's heads
   uint32_t pairs;      // n: pairs that are turned
   int32_t inverse;
   RotaryTable tab;
 };
 
-// Heads that a thread reads at a time.
-constexpr int rotary_batch(int elem_bytes) { return 16 / elem_bytes; }
+constexpr int kRotaryBatch = 8;  // heads that a thread reads at a time
 
 hipError_t launch_rotary(cqsa_dtype dt, bool adjacent, const RotaryArgs& a, hipStream_t s);
 

@@ -157,15 +157,16 @@ cqsa_status rotary_impl(const cqsa_rotary_s* p, const int32_t* pos, const cqsa_v
   a.H0 = uint32_t(x[0].H);
   a.H = uint32_t(heads);
   a.pairs = uint32_t(p->n);
-  a.chunks = uint32_t(p->n / 8);
-  a.units = in_place ? a.chunks : uint32_t(p->opts.d / 16);
+  const int32_t vec = int32_t(16 / elem_bytes(x[0].dtype));
+  a.chunks = uint32_t(p->n / vec);
+  a.units = in_place ? a.chunks : uint32_t(p->opts.d / (2 * vec));
   a.inverse = inverse;
   a.tab = p->tab;
   // A thread takes a batch of heads, fewer where that leaves under 2^18 threads
   // (4096 rows of 40 heads, bf16, d = 128: 5 heads each 16.9 us, 1 or 2 24.3;
   // 32768 rows of 32: 8 heads 83, 32 101).
-  const int64_t batch = rotary_batch(int(elem_bytes(x[0].dtype))), per = rows * a.units;
-  a.parts = uint32_t(std::max<int64_t>((a.H + batch - 1) / batch,
+  const int64_t per = rows * a.units;
+  a.parts = uint32_t(std::max<int64_t>((a.H + kRotaryBatch - 1) / kRotaryBatch,
                                        std::min<int64_t>(a.H, ((1 << 18) + per - 1) / per)));
   const int64_t per_row = int64_t(a.units) * a.parts;
   const int64_t slab = (int64_t(1) << 30) / per_row;  // rows of a launch; per_row <= 2^24
