@@ -67,9 +67,11 @@ struct AttendPlan {
 AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
 
 // The kernel for many rows (of 16 bits): rows of a work group, 32 a wave, with two
-// waves on a SIMD where their registers fit; tokens of a tile (64 KB of LDS for
-// two of them); launch.
-constexpr int attend_many_rows(int d) { return d <= 128 ? 256 : 128; }
+// waves on a SIMD where their registers fit (fp16 at d = 192 spills 14 of them and
+// takes 0.63 ms, with 4 waves 0.93; at d = 224 47 and 1.00 to 1.02 ms, but 0.23 to
+// 0.13 where sequences have 128 rows); tokens of a tile (64 KB of LDS for two of
+// them); launch.
+constexpr int attend_many_rows(bool f16, int d) { return f16 && d > 192 ? 128 : 256; }
 constexpr int attend_many_tokens(int d) { return d <= 128 ? 64 : 32; }
 hipError_t launch_attend_many(cqsa_dtype dt, const AttendArgs& a, const AttendPlan& p, hipStream_t s);
 

@@ -527,25 +527,30 @@ AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa
   const int parts = dt == CQSA_F32 ? 3 : (dt == CQSA_F16 ? 2 : 1);
   int64_t tiles = (max_len + 31) / 32;
   const int64_t units = B * H * ((rows + 15) / 16) * tiles;
-  // The kernel for many rows decodes a tile once for 256 rows (128 from d =
-  // 160), but walks its tiles with a barrier each, so it has to have many of
-  // them.  us, few and many, bf16 d = 128, 8 key heads: 2^16 units (4096 tokens,
-  // 1024 rows) 36.6 and 37.6, 2^17 (4096, 2048) 51.6 and 53.3, 2^17 (32 times
-  // 2048, 128 rows) 72.8 and 49.7, 2^18 (8192, 2048) 97.8 and 84.0; d = 256: 2^18
-  // 218.6 and 229.4, 2^20 886.8 and 808.5.  In fp32 its three parts leave no
-  // registers for a second wave (d = 128: 2^20 units 741.7 and 727.0, d = 256
-  // 1757 and 2450), so it is not built for that.
-  const bool many = dt != CQSA_F32 && rows > 64 && units >= (d <= 128 ? 1 << 17 : 1 << 19);
+  // The kernel for many rows decodes a tile once for 256 rows, but walks its tiles
+  // with a barrier each, so it has to have many of them.  us, few and many, bf16
+  // d = 128, 8 key heads: 2^16 units (4096 tokens, 1024 rows) 36.6 and 37.6, 2^17
+  // (4096, 2048) 51.6 and 53.3, 2^17 (32 times 2048, 128 rows) 72.8 and 49.7, 2^18
+  // (8192, 2048) 97.8 and 84.0; d = 192: 2^15 (2048, 1024) 37.7 and 41.5, 2^16 68.3
+  // and 51.9, 2^18 251 and 116; d = 256: 2^16 67.7 and 69.6, 2^18 241 and 156.  In
+  // fp16 at d = 256 and in fp32 the queries' parts leave too few registers (fp16
+  // 2^18 257 and 317; fp32 at d = 128 2^20 742 and 727, at d = 256 1757 and 2450),
+  // so it is not built for those.
+  const bool built = dt == CQSA_BF16 || (dt == CQSA_F16 && d < 256);
+  const bool many = built && rows > 64 && units >= (d <= 128 ? 1 << 17 : 1 << 16);
   if (many) {
     p.row_groups = 0;
-    p.row_tiles = int((rows + attend_many_rows(d) - 1) / attend_many_rows(d));
+    const int tall = attend_many_rows(dt == CQSA_F16, d);
+    p.row_tiles = int((rows + tall - 1) / tall);
     // one work group a CU: the number of splits whose rounds of 256 are the
-    // shortest in all, with 6 tiles' time for a round's start and end
+    // shortest in all, with 6 tiles' time for a round's start and end; more than 16
+    // only to fill one round (one key head, 256 rows over 262144 tokens, bf16, d =
+    // 128: 58 us, with 16 splits 473)
     tiles = (max_len + attend_many_tokens(d) - 1) / attend_many_tokens(d);
     const int64_t groups = B * H * p.row_tiles;
     int64_t best = 0;
     p.splits = 1;
-    for (int s = 1; s <= 16 && (s == 1 || tiles / s >= 8); ++s) {
+    for (int s = 1; (s <= 16 || groups * s <= 256) && (s == 1 || tiles / s >= 8); ++s) {
       const int64_t cost = (groups * s + 255) / 256 * ((tiles + s - 1) / s + 6);
       if (s == 1 || cost < best) best = cost, p.splits = s;
     }

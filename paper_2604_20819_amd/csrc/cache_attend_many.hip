@@ -341,7 +341,7 @@ namespace {
 
 template <typename T, int DB>
 void launch_one(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  constexpr int W = attend_many_rows(32 * DB) / 32;
+  constexpr int W = attend_many_rows(RowType<T>::kQuery == 2, 32 * DB) / 32;
   const dim3 grid(unsigned(int64_t(a.c.B) * a.c.H * p.row_tiles * p.splits)), block(64 * W);
   hipLaunchKernelGGL((cache_attend_many<T, DB, W, attend_many_tokens(32 * DB)>), grid, block, 0, s, a, p.row_tiles,
                      p.splits, p.min_chunk);
@@ -363,8 +363,13 @@ hipError_t launch_many(const AttendArgs& a, const AttendPlan& p, hipStream_t s) 
     CQSA_MANY(5)
     CQSA_MANY(6)
     CQSA_MANY(7)
-    CQSA_MANY(8)
 #undef CQSA_MANY
+    case 256:
+      if constexpr (RowType<T>::kQuery == 1) {
+        launch_one<T, 8>(a, p, s);
+        break;
+      }
+      [[fallthrough]];
     default:
       return hipErrorInvalidValue;
   }

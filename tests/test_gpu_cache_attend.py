@@ -190,6 +190,17 @@ def test_long_contexts(lens, n, G, B_pad):
     run(case, normal(case.g, (len(lens), n, G, d), "bf16"))
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 192), ("bf16", 256)])
+def test_many_rows_of_a_long_context(dtype, d):
+    """One key head's long context spread over the whole GPU, beside one that leaves most parts empty."""
+    need_gpu()
+    lens, n, G = (40001, 33), 25, 4
+    case = Case(71 + d, lens, 1, d, 256)
+    case.fill_tokens()
+    say("attend many long", dtype, d)
+    run(case, normal(case.g, (2, n, G, d), dtype), dtype=dtype, kind="many")
+
+
 @pytest.mark.parametrize("kind,G,dtype", [("few", 3, "bf16"), ("few", 3, "f32"), ("two", 1, "f16"), ("many", 3, "bf16")])
 def test_packed_rows(kind, G, dtype):
     """Ragged rows; rows of no sequence stay as they were, LSE's too."""
