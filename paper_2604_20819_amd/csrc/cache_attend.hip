@@ -397,8 +397,9 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
 // and channels (4 a lane), so that a row of many splits is not a chain of
 // loads.
 template <typename T, int WPR>
-__global__ void __launch_bounds__(256) cache_attend_join(const AttendArgs a, int per_seq, int splits) {
-  constexpr int RPG = 4 / WPR;  // rows of a work group
+__global__ void __launch_bounds__(WPR > 4 ? 64 * WPR : 256)
+    cache_attend_join(const AttendArgs a, int per_seq, int splits) {
+  constexpr int W = WPR > 4 ? WPR : 4, RPG = W / WPR;  // waves and rows of a work group
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = wave % WPR;
   const int b = blockIdx.x / per_seq;
@@ -407,8 +408,8 @@ __global__ void __launch_bounds__(256) cache_attend_join(const AttendArgs a, int
   const int64_t rows = int64_t(s.n) * a.Hq;
   const int lanes = c.d / 4, ways = 64 / lanes;  // lanes of a split, splits at a time
   const int way = lane / lanes, ch = 4 * (lane % lanes);
-  __shared__ float factor[4][kMaxSplits];
-  __shared__ f32x4 part[4][64];
+  __shared__ float factor[W][kMaxSplits];
+  __shared__ f32x4 part[W][64];
   for (int64_t i0 = int64_t(blockIdx.x % per_seq) * RPG; i0 < rows; i0 += int64_t(per_seq) * RPG) {
     const int64_t i = i0 + wave / WPR;
     const bool live = i < rows;
@@ -427,6 +428,7 @@ __global__ void __launch_bounds__(256) cache_attend_join(const AttendArgs a, int
         l += y * f;
         factor[wave][k] = y == 0.f ? 0.f : f;
       }
+      __builtin_amdgcn_wave_barrier();  // other lanes' factors
       l = sum_of_wave(l);
       if (way < ways) {
 #pragma unroll 4
@@ -493,15 +495,20 @@ hipError_t launch_few(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 template <typename T>
 hipError_t launch_join(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   const int64_t rows = int64_t(a.c.q_start ? a.c.max_q : a.c.rows) * a.Hq;
-  const bool wide = p.splits > 8;
-  int64_t per = wide ? rows : (rows + 3) / 4;
-  const int64_t most = (int64_t(1) << 23) / a.c.B;
+  // Waves a row: 16 where a wave would go round 64 times (one key head's 8 rows
+  // over 262144 tokens, d = 128, 512 splits: the call 25 us, with 4 waves 39; 16384
+  // tokens, d = 64, 64 splits: 12.9 and 10.5).
+  const int waves = p.splits * a.c.d >= 1 << 14 ? 16 : (p.splits > 8 ? 4 : 1);
+  int64_t per = waves > 1 ? rows : (rows + 3) / 4;
+  const int64_t most = (int64_t(1) << 21) / a.c.B;  // B is at most 2^20
   if (per > most) per = most;
-  const dim3 grid(unsigned(per * a.c.B)), block(256);
-  if (wide)
-    hipLaunchKernelGGL((cache_attend_join<T, 4>), grid, block, 0, s, a, int(per), p.splits);
+  const dim3 grid(unsigned(per * a.c.B));
+  if (waves == 16)
+    hipLaunchKernelGGL((cache_attend_join<T, 16>), grid, dim3(1024), 0, s, a, int(per), p.splits);
+  else if (waves == 4)
+    hipLaunchKernelGGL((cache_attend_join<T, 4>), grid, dim3(256), 0, s, a, int(per), p.splits);
   else
-    hipLaunchKernelGGL((cache_attend_join<T, 1>), grid, block, 0, s, a, int(per), p.splits);
+    hipLaunchKernelGGL((cache_attend_join<T, 1>), grid, dim3(256), 0, s, a, int(per), p.splits);
   return hipGetLastError();
 }
 
@@ -528,30 +535,35 @@ AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa
   int64_t tiles = (max_len + 31) / 32;
   const int64_t units = B * H * ((rows + 15) / 16) * tiles;
   // The kernel for many rows decodes a tile once for 256 rows, but walks its tiles
-  // with a barrier each, so it has to have many of them.  us, few and many, bf16
-  // d = 128, 8 key heads: 2^16 units (4096 tokens, 1024 rows) 36.6 and 37.6, 2^17
-  // (4096, 2048) 51.6 and 53.3, 2^17 (32 times 2048, 128 rows) 72.8 and 49.7, 2^18
-  // (8192, 2048) 97.8 and 84.0; d = 192: 2^15 (2048, 1024) 37.7 and 41.5, 2^16 68.3
-  // and 51.9, 2^18 251 and 116; d = 256: 2^16 67.7 and 69.6, 2^18 241 and 156.  In
-  // fp16 at d = 256 and in fp32 the queries' parts leave too few registers (fp16
-  // 2^18 257 and 317; fp32 at d = 128 2^20 742 and 727, at d = 256 1757 and 2450),
-  // so it is not built for those.
+  // with a barrier each, so it has to fill the GPU: unsplit, or with many tiles.
+  // us, few and many, bf16, 8 key heads: 64 sequences of 128 tokens, 512 rows, d =
+  // 128, 95 and 42, d = 256 195 and 82; 32 of 1000, 128 rows 33 and 28, d = 32 17
+  // and 18.  With splits, d = 128: 2^16 units (4096 tokens, 1024 rows) 36.0 and
+  // 38.1, 2^17 (4096, 2048) 51.5 and 54.4, 2^18 (8192, 2048) 97.8 and 84.0; d = 192:
+  // 2^15 (2048, 1024) 37.7 and 41.5, 2^16 68.3 and 51.9, 2^18 251 and 116; d = 256:
+  // 2^16 68.1 and 69.9, 2^18 227 and 162.  In fp16 at d = 256 and in fp32 the
+  // queries' parts leave too few registers (fp16 2^18 257 and 317; fp32 at d = 128
+  // 2^20 742 and 727, at d = 256 1757 and 2450), so it is not built for those.
   const bool built = dt == CQSA_BF16 || (dt == CQSA_F16 && d < 256);
-  const bool many = built && rows > 64 && units >= (d <= 128 ? 1 << 17 : 1 << 16);
+  const int tall = attend_many_rows(dt == CQSA_F16, d);
+  const int64_t row_tiles = (rows + tall - 1) / tall;
+  const bool many = built && rows > 64 && (B * H * row_tiles >= 256 || units >= (d <= 128 ? 1 << 17 : 1 << 16));
   if (many) {
     p.row_groups = 0;
-    const int tall = attend_many_rows(dt == CQSA_F16, d);
-    p.row_tiles = int((rows + tall - 1) / tall);
+    p.row_tiles = int(row_tiles);
     // one work group a CU: the number of splits whose rounds of 256 are the
-    // shortest in all, with 6 tiles' time for a round's start and end; more than 16
-    // only to fill one round (one key head, 256 rows over 262144 tokens, bf16, d =
-    // 128: 58 us, with 16 splits 473)
-    tiles = (max_len + attend_many_tokens(d) - 1) / attend_many_tokens(d);
+    // shortest in all, with 6 tiles' time for a round's start and end, and for a
+    // join its launch's and that of its parts, 4 d bytes a row written and read;
+    // more than 16 only to fill one round (one key head, 256 rows over 262144
+    // tokens, bf16, d = 128: 58 us, with 16 splits 473)
+    const int tokens = attend_many_tokens(d);
+    tiles = (max_len + tokens - 1) / tokens;
     const int64_t groups = B * H * p.row_tiles;
     int64_t best = 0;
     p.splits = 1;
     for (int s = 1; (s <= 16 || groups * s <= 256) && (s == 1 || tiles / s >= 8); ++s) {
-      const int64_t cost = (groups * s + 255) / 256 * ((tiles + s - 1) / s + 6);
+      int64_t cost = (groups * s + 255) / 256 * ((tiles + s - 1) / s + 6);
+      if (s > 1) cost += 2 + B * H * rows * s / (128 * tokens * parts);
       if (s == 1 || cost < best) best = cost, p.splits = s;
     }
     p.min_chunk = 8;

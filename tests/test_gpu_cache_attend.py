@@ -241,6 +241,55 @@ def test_given_up_pages_and_bad_entries(kind, rows):
         run(case, normal(case.g, (4, n, 2, d), "bf16"), kind=kind)
 
 
+@pytest.mark.parametrize("kind", ["few", "two", "many"])
+def test_starts_that_fall(kind):
+    """Rows that two sequences share get results of any; the others are right, and none of no
+    sequence is written."""
+    need_gpu()
+    lens, G, d = (60, 70, 80), 4, 64
+    case = Case(83, lens, 1, d, 32)
+    case.fill_tokens()
+    q = normal(case.g, (1, 60, G, d), "bf16")
+    batch = bounded(case, kind, q_start=torch.tensor([3, 30, 20, 55], dtype=torch.int32).cuda(), max_q=40)
+    O = torch.full_like(q, 9.0, device="cuda")
+    LSE = torch.full((1, G, 60), 9.0, device="cuda")
+    cq.cqsa_cache_attend(case.cache(), batch, q.cuda(), O, LSE)
+    o, l = O[0].cpu().double().numpy(), LSE[0].t().cpu().double().numpy()
+    for b, lo, hi, first, last in ((0, 3, 30, 3, 20), (2, 20, 55, 30, 55)):
+        ref = reference(case, synth.as_f64(q)[0, lo:hi], b, lens[b], True)
+        held("bf16", o[first:last], l[first:last], [x[first - lo:last - lo] for x in ref], lens[b])
+    for x in (o, l):
+        assert (x[:3] == 9).all() and (x[55:] == 9).all()
+
+
+def test_no_pages_and_no_tokens():
+    """A pool of no pages, and a table of no columns: nothing is seen."""
+    need_gpu()
+    empty = cq.Cache4(0, 2, 64, page_size=32)
+    lengths = torch.tensor([5, 0], dtype=torch.int32, device="cuda")
+    q = torch.ones((2, 3, 4, 64), dtype=torch.float16, device="cuda")
+    k, v = torch.full((2, 2, 3, 2, 64), 9.0, dtype=torch.float16, device="cuda")
+    for columns in (0, 1):
+        batch = cq.CacheBatch(torch.zeros((2, columns), dtype=torch.int32, device="cuda"), lengths)
+        O, LSE = torch.full_like(q, 9.0), torch.full((2, 4, 3), 9.0, device="cuda")
+        cq.cqsa_cache_write(empty, batch, k, v)
+        cq.cqsa_cache_attend(empty, batch, q, O, LSE)
+        assert (O == 0).all() and LSE.isneginf().all()
+        ko, vo = torch.full_like(k, 9.0), torch.full_like(v, 9.0)
+        cq.cqsa_cache_read(empty, batch, ko, vo)
+        assert (ko == 0).all() and (vo == 0).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f16", 224), ("bf16", 256)])
+def test_many_sequences_of_many_rows(dtype, d):
+    """Whole short prompts, whose work groups fill the GPU: the kernel for many rows without splits."""
+    need_gpu()
+    lens, n, H = tuple(80 - 7 * (i % 9) for i in range(64)), 80, 4
+    case = Case(89, lens, H, d, 32)
+    case.fill_tokens()
+    run(case, normal(case.g, (64, n, H, d), dtype), dtype=dtype)
+
+
 def test_lengths_out_of_range():
     need_gpu()
     case = Case(29, (96, 96, 96), 1, 64, 32)
