@@ -478,7 +478,9 @@ uint64_t cqsa_cache_page_bytes(int32_t page_size, int32_t H, int32_t d);
  * dropped, reading from it gives zeros and attention leaves its tokens out, so
  * such entries may stand for tokens that a caller has given up.
  * Values outside their range are taken as the nearest one allowed: lengths in
- * [0, max_len], q_start in [0, T] and not falling, n_b at most max_q. */
+ * [0, max_len], q_start in [0, T] and q_start[b + 1] from q_start[b] on, n_b at most
+ * max_q.  Where q_start falls, so that sequences share rows, a row of those gets
+ * results of any of them. */
 typedef struct {
   const int32_t* pages;   /* device [B, max_pages] */
   int64_t pages_stride;   /* elements between two sequences' tables, >= max_pages */
@@ -507,7 +509,7 @@ cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* bat
  * and dtype, Q itself or no element of it; LSE (or NULL): fp32 [B, H_q, L], the natural logarithm of the sum of the
  * exponentials of the scaled scores.  A row that sees nothing gets O = 0 and LSE =
  * -infinity.  A NaN in a token reaches only rows that see it.  scale <= 0 selects
- * 1 / sqrt(d).  Scores and the softmax are fp32 for every dtype.
+ * 1 / sqrt(d); scale log2(e) must be finite.  Scores and the softmax are fp32 for every dtype.
  * workspace: device memory of at least cqsa_cache_attend_workspace bytes, 16-byte aligned,
  * with any contents; NULL where that is 0.  Calls that may overlap, replays of captured
  * graphs among them, need workspaces of their own. */

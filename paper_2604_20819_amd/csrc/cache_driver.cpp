@@ -21,6 +21,7 @@ int page_log2_of(int32_t page_size) {
 }
 
 constexpr int32_t kMaxHeads = 65536;
+constexpr float kLog2e = 1.4426950408889634f;
 
 cqsa_status check_cache(const cqsa_cache* c, const std::string& what) {
   if (!c) return fail(CQSA_ERR_INVALID_ARG, what + "cache is NULL");
@@ -105,6 +106,7 @@ cqsa_status move_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa
   if (empty(*K) || b->B == 0) return CQSA_OK;
   if (int64_t(b->B) * c->H > (int64_t(1) << 23))
     return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences and heads than one launch takes");
+  if (!write && K->data == V->data) return fail(CQSA_ERR_INVALID_ARG, what + "K and V are one tensor");
   if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;
   CacheMoveArgs a{};
   a.c = args_of(c, b, *K);
@@ -135,14 +137,15 @@ cqsa_status check_attend(const cqsa_cache* c, const cqsa_cache_batch* b, const c
   if ((st = check_view(Q, "Q", c->d, false)) != CQSA_OK) return st;
   if ((st = check_rows(b, *Q, what)) != CQSA_OK) return st;
   if (empty(*Q) || b->B == 0) return CQSA_OK;
-  // Work groups have 256 threads or more, and a launch fewer than 2^32 of them.
+  // Work groups have up to 512 threads where they are many, and a launch fewer than
+  // 2^32 of them.
   const int64_t rows = int64_t(b->q_start ? b->max_q : Q->L) * (Q->H / c->H);
   const int64_t heads = int64_t(b->B) * c->H;
   if (rows > (int64_t(1) << 30) || heads > (int64_t(1) << 23) ||
       heads * ((rows + 15) / 16) > (int64_t(1) << 27))
     return fail(CQSA_ERR_UNSUPPORTED, what + "more rows than one launch takes");
   const AttendPlan p = attend_plan(c, b, *Q);
-  if (heads * p.row_tiles * p.splits > (int64_t(1) << 23))
+  if (heads * p.row_tiles * p.splits >= (int64_t(1) << 23))
     return fail(CQSA_ERR_UNSUPPORTED, what + "more rows than one launch takes");
   return CQSA_OK;
 }
@@ -156,7 +159,10 @@ cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   if ((st = check_view(O, "O", c->d, true)) != CQSA_OK) return st;
   if (!same_shape(*Q, *O)) return fail(CQSA_ERR_INVALID_ARG, what + "O differs from Q in shape or dtype");
   if (causal != 0 && causal != 1) return fail(CQSA_ERR_INVALID_ARG, what + "causal must be 0 or 1");
-  if (!std::isfinite(scale)) return fail(CQSA_ERR_INVALID_ARG, what + "scale must be finite");
+  if (!std::isfinite(scale * kLog2e))
+    return fail(CQSA_ERR_INVALID_ARG, what + "scale must be finite, in powers of two too");
+  if (!empty(*Q) && Q->data == O->data && !same_place(*Q, *O))
+    return fail(CQSA_ERR_INVALID_ARG, what + "O overlaps Q without being Q");
   if (empty(*Q) || b->B == 0) return CQSA_OK;
   if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;
   if (reinterpret_cast<uintptr_t>(LSE) % 4 != 0)
@@ -169,7 +175,7 @@ cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   a.Hq = int32_t(Q->H);
   a.G = int32_t(Q->H / c->H);
   a.causal = causal;
-  a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(float(c->d))) * 1.4426950408889634f;
+  a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(float(c->d))) * kLog2e;
   const AttendPlan p = attend_plan(c, b, *Q);
   const uint64_t need = attend_bytes(p, *Q);
   if (need > 0) {

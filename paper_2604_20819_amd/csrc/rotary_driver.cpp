@@ -53,12 +53,13 @@ __int128 extent(const cqsa_view& v) {
   auto reach = [](int64_t n, int64_t s) { return n > 1 ? __int128(n - 1) * s : __int128(0); };
   return reach(v.B, v.stride_b) + reach(v.L, v.stride_l) + reach(v.H, v.stride_h) + v.d;
 }
+}  // namespace
+
 bool same_place(const cqsa_view& x, const cqsa_view& y) {
   auto same = [](int64_t n, int64_t a, int64_t b) { return n == 1 || a == b; };
   return x.data == y.data && same(x.B, x.stride_b, y.stride_b) && same(x.L, x.stride_l, y.stride_l) &&
          same(x.H, x.stride_h, y.stride_h);
 }
-}  // namespace
 
 bool views_meet(const cqsa_view& x, const cqsa_view& y) {
   if (empty(x) || empty(y)) return false;
@@ -140,6 +141,8 @@ cqsa_status rotary_impl(const cqsa_rotary_s* p, const int32_t* pos, const cqsa_v
     if (!same && views_meet(x[k], y[k]))
       return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: y overlaps x without being x");
   }
+  if (n == 2 && !empty(y[0]) && y[0].data == y[1].data)
+    return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: the results are one tensor");
   if (heads > (1 << 20))
     return fail(CQSA_ERR_UNSUPPORTED, "cqsa_rotary: more than 2^20 heads");
   const int64_t rows = x[0].B * x[0].L;
@@ -163,7 +166,7 @@ cqsa_status rotary_impl(const cqsa_rotary_s* p, const int32_t* pos, const cqsa_v
   a.inverse = inverse;
   a.tab = p->tab;
   // A thread takes a batch of heads, fewer where that leaves under 2^18 threads
-  // (4096 rows of 40 heads, bf16, d = 128: 5 heads each 16.9 us, 1 or 2 24.3;
+  // (4096 rows of 40 heads, bf16, d = 128: 5 heads each 15.7 us, 1 or 2 24.3;
   // 32768 rows of 32: 8 heads 83, 32 101).
   const int64_t per = rows * a.units;
   a.parts = uint32_t(std::max<int64_t>((a.H + kRotaryBatch - 1) / kRotaryBatch,

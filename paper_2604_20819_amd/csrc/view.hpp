@@ -16,6 +16,8 @@ inline bool empty(const cqsa_view& v) { return v.B == 0 || v.L == 0 || v.H == 0;
 cqsa_status check_view(const cqsa_view* v, const char* name, int64_t d, bool written);
 // Whether two views have one shape and dtype.
 bool same_shape(const cqsa_view& x, const cqsa_view& y);
+// Whether two views of one shape have the same elements' addresses.
+bool same_place(const cqsa_view& x, const cqsa_view& y);
 // Whether the bytes that two views span meet.
 bool views_meet(const cqsa_view& x, const cqsa_view& y);
 

@@ -98,6 +98,8 @@ def test_rotary_calls_refused():
     refused(call([ok], [view(data=PTR + 16)]), "overlaps x")
     refused(call([ok, view(L=5)], [out, view(L=5, **far)], n=2), "share B, L")
     refused(call([ok, view(dtype=cq.CQSA_F16)], [out, view(dtype=cq.CQSA_F16, **far)], n=2), "share B, L")
+    refused(call([ok, ok], [ok, ok], n=2), "one tensor")
+    refused(call([ok, view(data=PTR + (1 << 31))], [out, out], n=2), "one tensor")
     assert call([view(B=0, data=None)], [view(B=0, data=None)]) == 0  # nothing to do
 
 
@@ -181,6 +183,8 @@ def test_more_of_attend_refused():
     refused(call(causal=2), "causal")
     refused(call(scale=float("nan")), "scale")
     refused(call(scale=float("inf")), "scale")
+    refused(call(scale=3e38), "scale")  # infinite as a factor of powers of two
+    refused(call(o=view(stride_h=3 * 64, stride_l=64)), "without being Q")
     refused(call(lse=PTR + 2), "LSE")
     refused(call(o=view(L=4, **far)), "O differs")
     refused(call(o=view(dtype=cq.CQSA_F32, **far)), "O differs")
@@ -228,12 +232,24 @@ def test_workspace_by_the_sizes_alone():
         refused(lib.cqsa_cache_attend(cache(), b, q, view(L=1, data=PTR + (1 << 32)), None, 1, 0.0, space, size, None), text)
 
 
+def test_workspace_of_many_rows():
+    """One key head's rows are split to fill the GPU, rows that fill it by themselves are not split."""
+    lib, n = cq.lib(), ctypes.c_uint64(7)
+    b = batch(B=1, max_pages=1 << 14, pages_stride=1 << 14, max_len=1 << 20)
+    assert lib.cqsa_cache_attend_workspace(cache(H=1), b, view(B=1, L=64), n) == 0
+    splits, rest = divmod(n.value, 64 * 4 * (64 + 4) * 4)
+    assert rest == 0 and 128 < splits <= 256
+    b = batch(B=64, max_len=128)
+    assert lib.cqsa_cache_attend_workspace(cache(H=4), b, view(B=64, L=128, H=16), n) == 0 and n.value == 0
+
+
 def test_write_and_read_views_refused():
     lib = cq.lib()
     for f in (lib.cqsa_cache_write, lib.cqsa_cache_read):
         refused(f(cache(), batch(), view(), view(L=4), None), "K and V differ")
         refused(f(cache(), batch(), view(), view(dtype=cq.CQSA_F32), None), "K and V differ")
     refused(lib.cqsa_cache_read(cache(), batch(), view(), view(stride_h=0), None), "overlaps itself")
+    refused(lib.cqsa_cache_read(cache(), batch(), view(), view(), None), "one tensor")
 
 
 # ---------------------------------------------------- the oracle, by itself
