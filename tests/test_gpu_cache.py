@@ -222,3 +222,18 @@ def test_captured_step():
         torch.cuda.synchronize()
         for got, x in ((ko, a), (vo, b)):
             assert np.array_equal(got.cpu().double().numpy(), o4.values(*o4.quantise(synth.as_f64(x))))
+
+
+def test_sequences_that_share_a_page():
+    """Two sequences write neighbouring tokens of one page, and of one tile, in one call."""
+    need_gpu()
+    H, d, page = 3, 96, 64
+    case = Case(6, (5, 41), H, d, page)
+    case.table[1] = case.table[0]
+    new = (5, 36)  # tokens 0 .. 4 and 5 .. 40
+    k, v = (normal(case.g, (1, sum(new), H, d), "bf16") for _ in range(2))
+    cache = case.cache()
+    cq.cqsa_cache_write(cache, case.batch(q_start=starts(new), max_q=max(new)), k.cuda(), v.cuda())
+    p, t = case.slots(1, 0, 41)
+    o4.write(case.data, page, synth.as_f64(k)[0], synth.as_f64(v)[0], p, t)
+    assert np.array_equal(cache.data.cpu().numpy(), case.data)

@@ -422,6 +422,39 @@ def test_captured_on_streams_and_repeated(n, lens, kind):
             assert torch.equal(O, got[0]) and torch.equal(LSE, got[1])
 
 
+@pytest.mark.parametrize("n,kind", [(1, "few"), (30, "many")])
+def test_two_calls_at_once(n, kind):
+    """Calls on two streams, and graphs captured without a workspace of the caller's, side by side."""
+    need_gpu()
+    G, d, jobs = 4, 64, []
+    for seed in (97, 101):
+        case = Case(seed, (6000, 900), 1, d, 64)
+        case.fill_tokens()
+        q = normal(case.g, (2, n, G, d), "bf16")
+        want, _ = run(case, q, kind=kind)
+        jobs.append((case.cache(), bounded(case, kind), q.cuda(), torch.empty_like(want), want))
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for s, (cache, batch, q, O, _) in zip(streams, jobs):
+            cq.cqsa_cache_attend(cache, batch, q, O, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(O, want) for _, _, _, O, want in jobs)
+    graphs = []
+    for s, (cache, batch, q, O, _) in zip(streams, jobs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            cq.cqsa_cache_attend(cache, batch, q, O)
+        O.zero_()
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(O, want) for _, _, _, O, want in jobs)
+
+
 def test_pages_beyond_four_gigabytes():
     need_gpu()
     H, d, page = 8, 128, 256
