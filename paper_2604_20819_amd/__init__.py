@@ -541,7 +541,15 @@ def cqsa_cache_page_bytes(page_size, H, d):
     return lib().cqsa_cache_page_bytes(page_size, H, d)
 
 
-class Cache4:
+class _Fixed:
+    """Made once: the C structure of a call holds the addresses of its tensors, whose
+    contents may change, but which no others can replace."""
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"a {type(self).__name__} is made once; make another, or copy into its tensors")
+
+
+class Cache4(_Fixed):
     """A paged 4-bit cache of keys and values (cqsa_cache): n_pages pages of
     page_size tokens of H heads.  data: a contiguous uint8 tensor to keep it in
     (None: a new one of zeros on `device`)."""
@@ -558,12 +566,11 @@ class Cache4:
             raise ValueError("data must be a contiguous uint8 tensor on a GPU")
         if data.numel() != n_pages * per:
             raise ValueError(f"data must have {n_pages} x {per} bytes")
-        self.n_pages, self.H, self.d, self.page_size = n_pages, H, d, page_size
-        self.data, self.device = data, data.device
-        self.view = cqsa_cache(data.data_ptr(), n_pages, page_size, H, d)
+        self.__dict__.update(n_pages=n_pages, H=H, d=d, page_size=page_size, data=data, device=data.device,
+                             view=cqsa_cache(data.data_ptr(), n_pages, page_size, H, d))
 
 
-class CacheBatch:
+class CacheBatch(_Fixed):
     """The sequences of a call (cqsa_cache_batch).  pages: int32 [B, max_pages];
     lengths: int32 [B], the tokens in the cache with the call's; q_start: int32
     [B + 1] for packed rows, then max_q bounds a sequence's rows.  max_len bounds
@@ -577,13 +584,13 @@ class CacheBatch:
         _device_array(lengths, "lengths", (B,))
         if q_start is not None:
             _device_array(q_start, "q_start", (B + 1,))
-        self.pages, self.lengths, self.q_start = pages, lengths, q_start
-        self.max_len, self.max_q, self.device = max_len, max_q, pages.device
-        if lengths.device != self.device or (q_start is not None and q_start.device != self.device):
+        device = pages.device
+        if lengths.device != device or (q_start is not None and q_start.device != device):
             raise ValueError("all tensors of a batch must live on one device")
-        self.view = cqsa_cache_batch(pages.data_ptr(), pages.stride(0) if B > 1 else n, lengths.data_ptr(),
-                                     q_start.data_ptr() if q_start is not None else None, B, n,
-                                     max_len, max_q)
+        view = cqsa_cache_batch(pages.data_ptr(), pages.stride(0) if B > 1 else n, lengths.data_ptr(),
+                                q_start.data_ptr() if q_start is not None else None, B, n, max_len, max_q)
+        self.__dict__.update(pages=pages, lengths=lengths, q_start=q_start, max_len=max_len, max_q=max_q,
+                             device=device, view=view)
 
     def _of(self, cache, t):
         """The descriptor for a cache and a tensor of rows: the bounds left open filled in."""

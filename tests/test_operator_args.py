@@ -243,6 +243,15 @@ def test_workspace_of_many_rows():
     assert lib.cqsa_cache_attend_workspace(cache(H=4), b, view(B=64, L=128, H=16), n) == 0 and n.value == 0
 
 
+def test_batches_and_caches_are_made_once():
+    """Their descriptors hold addresses, which an assignment would leave behind."""
+    for kind, names in ((cq.CacheBatch, ("lengths", "pages", "max_len")), (cq.Cache4, ("data", "n_pages"))):
+        x = object.__new__(kind)
+        for name in names:
+            with pytest.raises(AttributeError, match="made once"):
+                setattr(x, name, None)
+
+
 def test_write_and_read_views_refused():
     lib = cq.lib()
     for f in (lib.cqsa_cache_write, lib.cqsa_cache_read):
