@@ -542,12 +542,16 @@ AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa
   // 38.1, 2^17 (4096, 2048) 51.5 and 54.4, 2^18 (8192, 2048) 97.8 and 84.0; d = 192:
   // 2^15 (2048, 1024) 37.7 and 41.5, 2^16 68.3 and 51.9, 2^18 251 and 116; d = 256:
   // 2^16 68.1 and 69.9, 2^18 227 and 162.  In fp16 at d = 256 and in fp32 the
-  // queries' parts leave too few registers (fp16 2^18 257 and 317; fp32 at d = 128
-  // 2^20 742 and 727, at d = 256 1757 and 2450), so it is not built for those.
-  const bool built = dt == CQSA_BF16 || (dt == CQSA_F16 && d < 256);
+  // queries' parts leave too few registers: fp16 takes it only for short sequences
+  // (16 of 256, 1024 rows, 119 and 66, of 1024 252 and 246, of 4096 823 and 963; split,
+  // 2^18, 257 and 317), and for fp32 it is not built (d = 128 2^20 742 and 727, d =
+  // 256 1757 and 2450).
   const int tall = attend_many_rows(dt == CQSA_F16, d);
   const int64_t row_tiles = (rows + tall - 1) / tall;
-  const bool many = built && rows > 64 && (B * H * row_tiles >= 256 || units >= (d <= 128 ? 1 << 17 : 1 << 16));
+  const bool fills = B * H * row_tiles >= 256;
+  const bool many = dt != CQSA_F32 && rows > 64 &&
+                    (dt == CQSA_F16 && d == 256 ? fills && max_len <= 1024
+                                                : fills || units >= (d <= 128 ? 1 << 17 : 1 << 16));
   if (many) {
     p.row_groups = 0;
     p.row_tiles = int(row_tiles);

@@ -363,13 +363,8 @@ hipError_t launch_many(const AttendArgs& a, const AttendPlan& p, hipStream_t s) 
     CQSA_MANY(5)
     CQSA_MANY(6)
     CQSA_MANY(7)
+    CQSA_MANY(8)
 #undef CQSA_MANY
-    case 256:
-      if constexpr (RowType<T>::kQuery == 1) {
-        launch_one<T, 8>(a, p, s);
-        break;
-      }
-      [[fallthrough]];
     default:
       return hipErrorInvalidValue;
   }

@@ -280,7 +280,7 @@ def test_no_pages_and_no_tokens():
         assert (ko == 0).all() and (vo == 0).all()
 
 
-@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f16", 224), ("bf16", 256)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f16", 224), ("bf16", 256), ("f16", 256)])
 def test_many_sequences_of_many_rows(dtype, d):
     """Whole short prompts, whose work groups fill the GPU: the kernel for many rows without splits."""
     need_gpu()
