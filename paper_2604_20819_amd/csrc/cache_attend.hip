@@ -175,10 +175,11 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
 
   f32x4 o[NQ][DB][2];
   float m[NQ], l[NQ];  // m: the shift (0 before the first tile that is seen, with l = 0)
+  float lp[NQ];        // with weights in one part: their sum as rounded
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     m[n] = -INFINITY;
-    l[n] = 0.f;
+    l[n] = lp[n] = 0.f;
 #pragma unroll
     for (int k = 0; k < DB; ++k) o[n][k][0] = o[n][k][1] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -219,6 +220,7 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
         const float f = m[n] == -INFINITY ? 0.f : fast_exp2(m[n] - mn);
         m[n] = mn;
         l[n] *= f;
+        if constexpr (WP == 1) lp[n] *= f;
 #pragma unroll
         for (int k = 0; k < DB; ++k) o[n][k][0] *= f, o[n][k][1] *= f;
       }
@@ -233,7 +235,10 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
     }
     bf16x8 w[NQ][WP];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) split8<WP>(p[n], w[n]);
+    for (int n = 0; n < NQ; ++n) {
+      split8<WP>(p[n], w[n]);
+      if constexpr (WP == 1) lp[n] = sum8<BF16>(w[n][0], lp[n]);
+    }
     if (mixed) {
       // Tokens that no row of the work group sees may be any bytes: their
       // exponents become 0, so that they are finite (their weights are 0).  A
@@ -302,6 +307,7 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     l[n] = sum_of_quarters(l[n]);
+    if constexpr (WP == 1) lp[n] = sum_of_quarters(lp[n]);
     if (quarter == 0) {
       stat[wave][16 * n + col][0] = m[n];
       stat[wave][16 * n + col][1] = l[n];
@@ -315,7 +321,8 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
     for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w][16 * n + col][0]);
     // m is -inf where every score was (or none was seen): NaN that came by a
     // value or a score stays
-    const float f = m[n] == -INFINITY ? 1.f : fast_exp2(m[n] - top);
+    float f = m[n] == -INFINITY ? 1.f : fast_exp2(m[n] - top);
+    if constexpr (WP == 1) f *= one_part_factor(l[n], lp[n]);
 #pragma unroll
     for (int k = 0; k < DB; ++k) o[n][k][0] *= f, o[n][k][1] *= f;
     auto slot = [&](int w) { return (float*)lds + (w * 16 + col) * OSTRIDE + 8 * quarter; };

@@ -7,8 +7,9 @@
 // products exact; weights in 2 for fp16 and 3 for fp32, and for bf16 rows in 2
 // where there are few and the cache's bytes bound the call (2 to 3 % of its
 // time), else in 1, which adds to a result that is rounded to bf16 anyway about
-// as much as that rounding (error of the result against 64 bits 2.4e-3 with
-// one part, 1.7e-3 with two; two take 10 to 15 % more from 17 rows on).  v_mfma_scale_f32_16x16x128_f8f6f4 would take
+// as much as that rounding (error of the result against 64 bits 2.3e-3 with
+// one part, 1.7e-3 with two; two take 10 to 15 % more from 17 rows on); the result
+// is then divided by the sum of the weights as rounded (one_part_factor).  v_mfma_scale_f32_16x16x128_f8f6f4 would take
 // the keys' codes and exponents as they are and save their decoding, but it
 // drops bits of products that lie some 11 binades below a sum's largest (a
 // score off by 2^-13 of its largest product, measured), and queries in e4m3
@@ -149,6 +150,15 @@ __device__ __forceinline__ float sum_of_wave(float x) {
   for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
   return x;
 }
+
+// What a row's unnormalised result is multiplied by where its weights enter the
+// product in one part: then it goes with the sum of the weights as rounded, lp,
+// but is divided by (and joined with others by) their exact sum l, which is LSE's.
+// Without it weights that all round the same way, as near-uniform attention has
+// them, would put the result off by up to a half step of bf16.  The second sum
+// costs 1 to 4 % from d = 96 on (4096 rows over 32768 tokens, d = 128: 1002 us,
+// without 976) and 7 to 9 % at d = 64 and 32.
+__device__ __forceinline__ float one_part_factor(float l, float lp) { return lp == 0.f ? 1.f : l / lp; }
 
 // Tokens that a row sees.
 __device__ __forceinline__ int seen_by(const Seq& s, int causal, int token) {

@@ -173,6 +173,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[k][r] = 0.f;
   float m = -INFINITY, l = 0.f;
+  float lp = 0.f;  // with weights in one part: their sum as rounded
 
   auto compute = [&](int t, int buf, int dead) {
     const char* kl = lds[buf] + lane * 16;
@@ -212,6 +213,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1)
       const float f = m == -INFINITY ? 0.f : fast_exp2(m - mn);
       m = mn;
       l *= f;
+      if constexpr (WP == 1) lp *= f;
 #pragma unroll
       for (int k = 0; k < DB; ++k)
 #pragma unroll
@@ -256,6 +258,7 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1)
         for (int r = 0; r < 8; ++r) p[r] = x[g][8 * st + r];
         bf16x8 w[WP];
         split8<WP>(p, w);
+        if constexpr (WP == 1) lp = sum8<BF16>(w[0], lp);
 #pragma unroll
         for (int k = 0; k < DB; ++k) {
           const bf16x8 vv = *(const bf16x8*)(vl + ((g * DB + k) * 2 + st) * 1024);
@@ -297,7 +300,15 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1)
   }
 
   l += swap_halves(l);
+  const float other = WP == 1 ? swap_halves(lp) : 0.f;
   if (myrow >= rows) return;
+  if constexpr (WP == 1) {
+    const float f = one_part_factor(l, lp + other);
+#pragma unroll
+    for (int k = 0; k < DB; ++k)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[k][r] *= f;
+  }
   const int64_t flat = (tb * a.Hq + hq) * int64_t(c.rows) + s.row0 + tok;
   if (splits == 1) {
     const float inv = l == 0.f ? 1.f : 1.f / l;
