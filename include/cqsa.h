@@ -522,6 +522,18 @@ cqsa_status cqsa_cache_attend(const cqsa_cache* cache, const cqsa_cache_batch* b
 cqsa_status cqsa_cache_attend_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,
                                         const cqsa_view* Q, uint64_t* bytes);
 
+/* How cqsa_cache_attend launches a call. */
+typedef struct {
+  int32_t many;   /* 1: the kernel for many rows a sequence, 0: that for few */
+  int32_t rows;   /* rows of a sequence and key head that a work group takes */
+  int32_t waves;  /* waves of a work group */
+  int32_t splits; /* work groups that share such rows' tokens; from 2 on a second kernel joins them */
+} cqsa_attend_launch;
+/* Host only: the launch of such a call, by the sizes of its arguments alone; all 0 where the
+ * call has no rows. */
+cqsa_status cqsa_cache_attend_launch(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                                     const cqsa_view* Q, cqsa_attend_launch* out);
+
 /* Route the library's device workspace through a caller allocator (e.g. a
  * framework's caching allocator).  alloc(bytes, ctx) returns device memory or
  * NULL (reported as CQSA_ERR_DEVICE_OOM); release(ptr, ctx) frees it.  Passing

@@ -107,6 +107,11 @@ class cqsa_cache_batch(ctypes.Structure):
                 ("max_q", ctypes.c_int32)]
 
 
+class cqsa_attend_launch(ctypes.Structure):
+    _fields_ = [("many", ctypes.c_int32), ("rows", ctypes.c_int32), ("waves", ctypes.c_int32),
+                ("splits", ctypes.c_int32)]
+
+
 _V, _C, _CB = (ctypes.POINTER(x) for x in (cqsa_view, cqsa_cache, cqsa_cache_batch))
 
 # Every symbol include/cqsa.h declares, with its ctypes signature.
@@ -160,6 +165,7 @@ _SIGS = {
                                          ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64,
                                          ctypes.c_void_p]),
     "cqsa_cache_attend_workspace": (ctypes.c_int, [_C, _CB, _V, ctypes.POINTER(ctypes.c_uint64)]),
+    "cqsa_cache_attend_launch": (ctypes.c_int, [_C, _CB, _V, ctypes.POINTER(cqsa_attend_launch)]),
     "cqsa_set_allocator": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "cqsa_set_timing": (ctypes.c_int, [ctypes.c_int32]),
     "cqsa_set_tile_counting": (ctypes.c_int, [ctypes.c_int32]),
@@ -633,6 +639,15 @@ def cqsa_cache_attend_workspace(cache, batch, Q):
     _check(_call("cqsa_cache_attend_workspace")(cache.view, batch._of(cache, Q), _view(Q, device), n),
            "cqsa_cache_attend_workspace")
     return _torch().empty(n.value, dtype=_torch().uint8, device=device) if n.value else None
+
+
+def cqsa_cache_attend_launch(cache, batch, Q):
+    """How cqsa_cache_attend launches a call with arguments of these sizes
+    (cqsa_attend_launch: many, rows, waves, splits)."""
+    out = cqsa_attend_launch()
+    _check(_call("cqsa_cache_attend_launch")(cache.view, batch._of(cache, Q), _view(Q, _cache_device(cache, batch)), out),
+           "cqsa_cache_attend_launch")
+    return out
 
 
 def _workspace_on(stream, cache, batch, Q):

@@ -250,4 +250,23 @@ cqsa_status cqsa_cache_attend_workspace(const cqsa_cache* cache, const cqsa_cach
   CQSA_ENTRY("cqsa_cache_attend_workspace", workspace_impl(cache, batch, Q, bytes))
 }
 
+static cqsa_status launch_impl(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                               const cqsa_view* Q, cqsa_attend_launch* out) {
+  const std::string what = "cqsa_cache_attend_launch: ";
+  if (!out) return fail(CQSA_ERR_INVALID_ARG, what + "out is NULL");
+  *out = cqsa_attend_launch{};
+  const cqsa_status st = check_attend(cache, batch, Q, what);
+  if (st != CQSA_OK || empty(*Q) || batch->B == 0) return st;
+  const AttendPlan p = attend_plan(cache, batch, *Q);
+  const bool many = p.row_groups == 0;
+  const int rows = many ? attend_many_rows(Q->dtype == CQSA_F16, cache->d) : 16 * p.row_groups;
+  *out = {many, rows, many ? rows / 32 : p.waves, p.splits};
+  return CQSA_OK;
+}
+
+cqsa_status cqsa_cache_attend_launch(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                                     const cqsa_view* Q, cqsa_attend_launch* out) {
+  CQSA_ENTRY("cqsa_cache_attend_launch", launch_impl(cache, batch, Q, out))
+}
+
 }  // extern "C"

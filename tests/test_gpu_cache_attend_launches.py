@@ -1,0 +1,136 @@
+"""Attention over the 4-bit cache on the GPU through launches that are named and checked:
+work groups of 8, 12 and 16 waves, and two groups of 16 rows a wave.  Bounds as in
+tests/test_gpu_cache_attend.py."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_20819_amd as cq
+from oracle import cache4 as o4
+from paper_2604_20819_amd import synth
+from tests.gpu_util import need_gpu, say
+from tests.op_util import Case, normal
+from tests.test_gpu_cache_attend import bounded, held, reference, run
+
+pytestmark = pytest.mark.gpu
+
+
+def launch(case, q, kind="few", **kw):
+    return cq.cqsa_cache_attend_launch(case.cache(), bounded(case, kind, **kw), q.cuda())
+
+
+WAVES = {"bf16": {32: 16, 64: 16, 96: 16, 128: 12, 160: 12, 192: 8, 224: 8, 256: 8},
+         "f16": {32: 16, 64: 16, 96: 12, 128: 12, 160: 8, 192: 8, 224: 8, 256: 8},
+         "f32": {32: 16, 64: 16, 96: 12, 128: 8, 160: 8, 192: 8}}
+
+
+@pytest.mark.parametrize("dtype,d", [(t, d) for t in WAVES for d in WAVES[t]])
+def test_work_groups_that_fill_a_cu(dtype, d):
+    """More than 128 sequences of few rows: their waves' states are joined in LDS, in halves.  One
+    sequence is long enough for every wave, others leave waves without a tile, one has none."""
+    need_gpu()
+    lens = (1000, 0, 1, 300, 33) + tuple(5 + i % 60 for i in range(135))
+    case = Case(d, lens, 1, d, 64)
+    case.fill_tokens()
+    q = normal(case.g, (len(lens), 3, 2, d), dtype)
+    say("attend wide", dtype, d)
+    x = launch(case, q)
+    assert (x.many, x.rows, x.waves, x.splits) == (0, 16, WAVES[dtype][d], 1)
+    run(case, q, dtype=dtype)
+    run(case, q[:, :1].contiguous(), dtype=dtype, causal=False)
+
+
+def two_groups(case, q):
+    x = launch(case, q, "two")
+    assert (x.many, x.rows) == (0, 32) and x.splits > 1
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 128)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_two_groups_query_that_is_not_finite(dtype, d, bad):
+    """Its own row is NaN, the other rows keep their bits."""
+    need_gpu()
+    case = Case(37, (90, 200), 2, d, 32)
+    case.fill_tokens()
+    q = normal(case.g, (2, 20, 6, d), dtype)
+    two_groups(case, q)
+    O, LSE = run(case, q, kind="two", dtype=dtype)
+    q2 = q.clone()
+    q2[1, 7, 4, 50] = bad
+    O2, LSE2 = run(case, q2, check=False, kind="two")
+    assert O2[1, 7, 4].isnan().all() and LSE2[1, 4, 7].isnan()
+    O2[1, 7, 4], LSE2[1, 4, 7] = O[1, 7, 4], LSE[1, 4, 7]
+    assert torch.equal(O2, O) and torch.equal(LSE2, LSE)
+
+
+def test_two_groups_result_over_the_queries():
+    need_gpu()
+    case = Case(67, (300, 65), 2, 64, 64)
+    case.fill_tokens()
+    q = normal(case.g, (2, 10, 8, 64), "bf16")
+    two_groups(case, q)
+    O, _ = run(case, q, kind="two")
+    x = q.cuda()
+    cq.cqsa_cache_attend(case.cache(), bounded(case, "two"), x, x)
+    assert torch.equal(x, O)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_two_groups_not_a_number_reaches_only_rows_that_see_it(dtype):
+    need_gpu()
+    n, G, d = 33, 3, 64
+    for what, at in (("k", 175), ("v", 175), ("v", 199), ("k", 199), ("v", 40)):
+        case = Case(31, (200,), 4, d, 64)
+        rows = case.fill_tokens()
+        q = normal(case.g, (1, n, 4 * G, d), dtype)
+        if what == "k" and at == 175:
+            two_groups(case, q)
+        O, LSE = run(case, q, kind="two", dtype=dtype)
+        k, v = (x.copy() for x in rows[0])
+        (k if what == "k" else v)[at, :, 35] = np.nan if at == 175 else np.inf
+        p, t = case.slots(0, 0, 200)
+        o4.write(case.data, 64, k, v, p, t)
+        O2, LSE2 = run(case, q, check=False, kind="two")
+        for i in range(n):
+            if at > 200 - n + i:
+                assert torch.equal(O2[0, i], O[0, i]) and torch.equal(LSE2[0, :, i], LSE[0, :, i])
+            elif what == "k":
+                assert O2[0, i].isnan().all() and LSE2[0, :, i].isnan().all()
+            else:
+                assert O2[0, i, :, 32:].isnan().all()
+                assert torch.equal(O2[0, i, :, :32], O[0, i, :, :32])
+                assert torch.equal(LSE2[0, :, i], LSE[0, :, i])
+
+
+def test_two_groups_captured():
+    """Replays follow the lengths and rows on the device, with a workspace of any contents."""
+    need_gpu()
+    H, G, d, n, lens = 2, 4, 64, 10, (700, 64)
+    case = Case(53, lens, H, d, 64)
+    case.fill_tokens()
+    cache, batch = case.cache(), bounded(case, "two")
+    q = normal(case.g, (2, n, H * G, d), "bf16").cuda()
+    two_groups(case, q)
+    O, LSE = torch.empty_like(q), torch.empty((2, H * G, n), device="cuda")
+    space = cq.cqsa_cache_attend_workspace(cache, batch, q)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        cq.cqsa_cache_attend(cache, batch, q, O, LSE, workspace=space)
+    for cut in (0, 1, 29):
+        now = [max(x - cut, 0) for x in lens]
+        batch.lengths.copy_(torch.tensor(now, dtype=torch.int32))
+        fresh = normal(case.g, (2, n, H * G, d), "bf16")
+        q.copy_(fresh)
+        space.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = O.clone(), LSE.clone()
+        for b, x in enumerate(now):
+            ref = reference(case, synth.as_f64(fresh)[b], b, x, True)
+            held("bf16", O[b].cpu().double().numpy(), LSE[b].t().cpu().double().numpy(), ref, max(x, 1))
+        O.zero_()
+        cq.cqsa_cache_attend(cache, batch, q, O, LSE, workspace=space)
+        torch.cuda.synchronize()
+        assert torch.equal(O, got[0]) and torch.equal(LSE, got[1])

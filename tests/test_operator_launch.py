@@ -1,0 +1,43 @@
+"""How attention over the 4-bit cache is launched, by its sizes alone (no GPU)."""
+import ctypes
+
+import pytest
+
+import paper_2604_20819_amd as cq
+from tests.test_operator_args import PTR, batch, cache, refused, view
+
+
+def launch(c, b, q):
+    out = cq.cqsa_attend_launch(7, 7, 7, 7)
+    assert cq.lib().cqsa_cache_attend_launch(c, b, q, out) == 0, cq.lib().cqsa_last_error()
+    return out
+
+
+def long_batch(B=1, max_len=1 << 20, **kw):
+    pages = -(-max_len // 64)
+    return batch(B=B, max_pages=pages, pages_stride=pages, max_len=max_len, **kw)
+
+
+@pytest.mark.parametrize("dtype", [cq.CQSA_BF16, cq.CQSA_F16, cq.CQSA_F32])
+@pytest.mark.parametrize("d", [32, 96, 128, 160, 256])
+def test_workspace_goes_by_the_splits(dtype, d):
+    n = ctypes.c_uint64()
+    for B, H, G, L, length in ((1, 1, 1, 1, 100), (1, 8, 2, 1, 1 << 20), (64, 8, 4, 1, 1 << 14), (1, 4, 4, 4096, 1 << 15),
+                               (200, 1, 1, 1, 1000), (2, 2, 2, 20, 1 << 17), (64, 4, 1, 100, 200)):
+        c, b, q = cache(H=H, d=d), long_batch(B, length), view(B=B, L=L, H=H * G, d=d, dtype=dtype)
+        x = launch(c, b, q)
+        assert cq.lib().cqsa_cache_attend_workspace(c, b, q, n) == 0
+        assert n.value == (B * L * H * G * x.splits * (d + 4) * 4 if x.splits > 1 else 0)
+        assert x.rows in ((128, 256) if x.many else (16, 32)) and x.splits >= 1
+        assert x.waves == x.rows // 32 if x.many else x.waves in (4, 8, 12, 16)
+        assert not (x.many and (dtype == cq.CQSA_F32 or L * G <= 64))
+
+
+def test_refused_and_empty():
+    lib, out = cq.lib(), cq.cqsa_attend_launch(7, 7, 7, 7)
+    refused(lib.cqsa_cache_attend_launch(cache(), batch(), view(), None), "out is NULL")
+    refused(lib.cqsa_cache_attend_launch(cache(), batch(B=5), view(), out), "B differs")
+    assert (out.many, out.rows, out.waves, out.splits) == (0, 0, 0, 0)
+    x = launch(cache(), batch(), view(L=0, data=None))
+    assert (x.many, x.rows, x.waves, x.splits) == (0, 0, 0, 0)
+    assert launch(cache(), batch(), view(data=PTR)).rows == 16
