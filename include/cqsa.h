@@ -512,7 +512,11 @@ cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* bat
  * 1 / sqrt(d); scale log2(e) must be finite.  Scores and the softmax are fp32 for every dtype.
  * workspace: device memory of at least cqsa_cache_attend_workspace bytes, 16-byte aligned,
  * with any contents; NULL where that is 0.  Calls that may overlap, replays of captured
- * graphs among them, need workspaces of their own. */
+ * graphs among them, need workspaces of their own.
+ * B sequences of n rows, or at most max_q packed ones, are launched as B H ceil(n (H_q / H) / 16)
+ * tiles, whether they all have that many rows or not: a bound far above them costs time (some
+ * 1.5 us for every 1000 tiles without rows), and more than 2^27 tiles, or 2^23 sequences and
+ * heads, are CQSA_ERR_UNSUPPORTED. */
 cqsa_status cqsa_cache_attend(const cqsa_cache* cache, const cqsa_cache_batch* batch,
                               const cqsa_view* Q, const cqsa_view* O, float* LSE, int32_t causal,
                               float scale, void* workspace, uint64_t workspace_bytes,

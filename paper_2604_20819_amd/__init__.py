@@ -579,8 +579,9 @@ class Cache4(_Fixed):
 class CacheBatch(_Fixed):
     """The sequences of a call (cqsa_cache_batch).  pages: int32 [B, max_pages];
     lengths: int32 [B], the tokens in the cache with the call's; q_start: int32
-    [B + 1] for packed rows, then max_q bounds a sequence's rows.  max_len bounds
-    the lengths (0: the table's tokens, once a cache says how many)."""
+    [B + 1] for packed rows, then max_q bounds a sequence's rows (0: all that the
+    tensors have; the launch goes by it, so single tokens want max_q=1).  max_len
+    bounds the lengths (0: the table's tokens, once a cache says how many)."""
 
     def __init__(self, pages, lengths, q_start=None, max_len=0, max_q=0):
         if pages.dim() != 2 or pages.dtype != _torch().int32 or not pages.is_cuda or \

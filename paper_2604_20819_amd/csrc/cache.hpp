@@ -66,6 +66,18 @@ struct AttendPlan {
 // rows: the most that a sequence and key head has.
 AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
 
+// Work groups of a launch of attention, with their splits: a call has at most this many
+// tiles of 16 rows, and is split only where 32 or 256 rows a work group, or a GPU that
+// they do not fill, leave as much room.
+constexpr int64_t kMaxGroups = int64_t(1) << 27;
+// They lie over two dimensions of the grid, the first 2^21 wide where there is a second,
+// since one has fewer than 2^32 threads.
+constexpr int kGridLog2 = 21;
+inline dim3 attend_grid(int64_t groups) {
+  const int64_t x = int64_t(1) << kGridLog2;
+  return groups <= x ? dim3(unsigned(groups)) : dim3(unsigned(x), unsigned((groups + x - 1) / x));
+}
+
 // The kernel for many rows (of 16 bits): rows of a work group, 32 a wave, with two
 // waves on a SIMD where their registers fit (fp16 at d = 192 spills 14 of them and
 // takes 0.63 ms, with 4 waves 0.93; at d = 224 47 and 1.00 to 1.02 ms, but 0.23 to

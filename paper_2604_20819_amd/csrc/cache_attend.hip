@@ -55,12 +55,13 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
   // Work groups go round the XCDs in this order: neighbours are other heads and
   // sequences, so that the splits of a sequence, the last of which may be
   // short, do not load one XCD more than another.
-  int id = blockIdx.x;
+  int id = (blockIdx.y << kGridLog2) + blockIdx.x;
   const int h = id % c.H;
   id /= c.H;
   const int b = id % c.B;
   id /= c.B;
   const int rt = id % row_tiles, sp = id / row_tiles;
+  if (sp >= splits) return;  // behind the last one, where the grid has two dimensions
   const Seq s = sequence(c, b);
   const int rows = s.n * a.G, r0 = rt * ROWS;  // at most 2^31: checked on the host
   if (r0 >= rows) return;
@@ -465,15 +466,15 @@ namespace {
 
 template <typename T, int NQ, int DB>
 void launch_waves(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  const unsigned grid = unsigned(int64_t(a.c.B) * a.c.H * p.row_tiles * p.splits);
+  const dim3 grid = attend_grid(int64_t(a.c.B) * a.c.H * p.row_tiles * p.splits);
   constexpr int W = 4 * few_waves(RowType<T>::kQuery, DB, 1);
   if constexpr (NQ == 1 && W > 4)
     if (p.waves > 4) {
-      hipLaunchKernelGGL((cache_attend_few<T, DB, 1, W>), dim3(grid), dim3(64 * W), 0, s, a, p.row_tiles, p.splits,
+      hipLaunchKernelGGL((cache_attend_few<T, DB, 1, W>), grid, dim3(64 * W), 0, s, a, p.row_tiles, p.splits,
                          p.min_chunk);
       return;
     }
-  hipLaunchKernelGGL((cache_attend_few<T, DB, NQ, 4>), dim3(grid), dim3(256), 0, s, a, p.row_tiles, p.splits,
+  hipLaunchKernelGGL((cache_attend_few<T, DB, NQ, 4>), grid, dim3(256), 0, s, a, p.row_tiles, p.splits,
                      p.min_chunk);
 }
 

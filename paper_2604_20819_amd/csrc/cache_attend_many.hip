@@ -46,12 +46,13 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1)
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the rows that see most first
-  int id = blockIdx.x;
+  int id = (blockIdx.y << kGridLog2) + blockIdx.x;
   const int h = id % c.H;
   id /= c.H;
   const int b = id % c.B;
   id /= c.B;
   const int sp = id % splits, rt = row_tiles - 1 - id / splits;
+  if (rt < 0) return;  // behind the last one, where the grid has two dimensions
   const Seq s = sequence(c, b);
   const int rows = s.n * a.G, r0 = rt * ROWS;
   if (r0 >= rows) return;
@@ -353,7 +354,7 @@ namespace {
 template <typename T, int DB>
 void launch_one(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   constexpr int W = attend_many_rows(RowType<T>::kQuery == 2, 32 * DB) / 32;
-  const dim3 grid(unsigned(int64_t(a.c.B) * a.c.H * p.row_tiles * p.splits)), block(64 * W);
+  const dim3 grid = attend_grid(int64_t(a.c.B) * a.c.H * p.row_tiles * p.splits), block(64 * W);
   hipLaunchKernelGGL((cache_attend_many<T, DB, W, attend_many_tokens(32 * DB)>), grid, block, 0, s, a, p.row_tiles,
                      p.splits, p.min_chunk);
 }

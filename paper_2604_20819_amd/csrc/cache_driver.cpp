@@ -137,15 +137,9 @@ cqsa_status check_attend(const cqsa_cache* c, const cqsa_cache_batch* b, const c
   if ((st = check_view(Q, "Q", c->d, false)) != CQSA_OK) return st;
   if ((st = check_rows(b, *Q, what)) != CQSA_OK) return st;
   if (empty(*Q) || b->B == 0) return CQSA_OK;
-  // Work groups have up to 512 threads where they are many, and a launch fewer than
-  // 2^32 of them.
   const int64_t rows = int64_t(b->q_start ? b->max_q : Q->L) * (Q->H / c->H);
   const int64_t heads = int64_t(b->B) * c->H;
-  if (rows > (int64_t(1) << 30) || heads > (int64_t(1) << 23) ||
-      heads * ((rows + 15) / 16) > (int64_t(1) << 27))
-    return fail(CQSA_ERR_UNSUPPORTED, what + "more rows than one launch takes");
-  const AttendPlan p = attend_plan(c, b, *Q);
-  if (heads * p.row_tiles * p.splits >= (int64_t(1) << 23))
+  if (rows > (int64_t(1) << 30) || heads > (int64_t(1) << 23) || heads * ((rows + 15) / 16) > kMaxGroups)
     return fail(CQSA_ERR_UNSUPPORTED, what + "more rows than one launch takes");
   return CQSA_OK;
 }

@@ -134,3 +134,27 @@ def test_two_groups_captured():
         cq.cqsa_cache_attend(cache, batch, q, O, LSE, workspace=space)
         torch.cuda.synchronize()
         assert torch.equal(O, got[0]) and torch.equal(LSE, got[1])
+
+
+@pytest.mark.parametrize("dtype,B,G,chunk", [("f32", 1024, 4, 1100), ("bf16", 2048, 8, 300)])
+def test_more_work_groups_than_one_dimension_takes(dtype, B, G, chunk):
+    """A chunk beside single tokens of many sequences, max_q far above both: 2^24 work groups of the
+    kernel for few rows, 2^22 of that for many.  Rows behind the last sequence stay as they were."""
+    need_gpu()
+    H, d, T = 8, 32, 8192
+    lens = (chunk + 50,) + tuple(b % 7 for b in range(1, B))
+    case = Case(B, lens, H, d, 32)
+    case.fill_tokens()
+    start = np.concatenate([[0], chunk + np.arange(B)]).astype(np.int32)
+    q = normal(case.g, (1, T, H * G, d), dtype)
+    batch = case.batch(q_start=torch.from_numpy(start).cuda(), max_q=T)
+    say("attend wide grid", dtype, B, G, chunk)
+    x = cq.cqsa_cache_attend_launch(case.cache(), batch, q.cuda())
+    assert x.many == (dtype == "bf16") and B * H * (T * G // x.rows) * x.splits > 1 << 21
+    O, LSE = torch.full_like(q, 9.0, device="cuda"), torch.full((1, H * G, T), 9.0, device="cuda")
+    cq.cqsa_cache_attend(case.cache(), batch, q.cuda(), O, LSE)
+    o, l = O[0].cpu().double().numpy(), LSE[0].t().cpu().double().numpy()
+    for b in [0] + list(range(1, B, 97)) + [B - 1]:
+        r = slice(start[b], start[b + 1])
+        held(dtype, o[r], l[r], reference(case, synth.as_f64(q[:, r].contiguous())[0], b, lens[b], True), max(lens[b], 1))
+    assert (o[start[-1]:] == 9).all() and (l[start[-1]:] == 9).all()

@@ -41,3 +41,13 @@ def test_refused_and_empty():
     x = launch(cache(), batch(), view(L=0, data=None))
     assert (x.many, x.rows, x.waves, x.splits) == (0, 0, 0, 0)
     assert launch(cache(), batch(), view(data=PTR)).rows == 16
+
+
+def test_ragged_batches_are_not_refused_by_rows_that_no_sequence_has():
+    """A chunk of 8192 rows beside 1023 single tokens: the grid that max_q asks for has 2^24 work
+    groups, more than one dimension of a grid takes."""
+    for dtype, most in ((cq.CQSA_BF16, 1 << 20), (cq.CQSA_F32, 1 << 24)):
+        c, b = cache(H=8), long_batch(1024, 1 << 14, q_start=PTR, max_q=8192)
+        q = view(B=1, L=8192 + 1023, H=32, dtype=dtype)
+        x = launch(c, b, q)
+        assert x.splits * 1024 * 8 * 8192 * 4 // x.rows == most
