@@ -499,6 +499,7 @@ cqsa_status cqsa_cache_write(const cqsa_cache* cache, const cqsa_cache_batch* ba
                              const cqsa_view* K, const cqsa_view* V, void* hip_stream);
 /* The values that the cache holds for the call's rows, into K and V (same shape and dtype):
  * what cqsa_cache_write wrote, or with n_b = lengths[b] whole sequences for cqsa_forward.
+ * K and V share no element (they may be parts of one buffer); this is checked.
  * Exact in bf16 and fp32, rounded to nearest even in fp16.  Rows before position 0 are zero. */
 cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* batch,
                             const cqsa_view* K, const cqsa_view* V, void* hip_stream);
@@ -506,7 +507,7 @@ cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* bat
 /* Attention of the call's rows Q (H_q heads, a multiple of the cache's H; head h reads the
  * cache's head h / (H_q / H)) over their sequences' cached tokens: with causal = 1 row i of
  * sequence b sees positions 0 ... lengths[b] - n_b + i, with 0 all of them.  O: Q's shape
- * and dtype, Q itself or no element of it; LSE (or NULL): fp32 [B, H_q, L], the natural logarithm of the sum of the
+ * and dtype, Q itself or no element of it (which is checked); LSE (or NULL): fp32 [B, H_q, L], the natural logarithm of the sum of the
  * exponentials of the scaled scores.  A row that sees nothing gets O = 0 and LSE =
  * -infinity.  A NaN in a token reaches only rows that see it.  scale <= 0 selects
  * 1 / sqrt(d); scale log2(e) must be finite.  Scores and the softmax are fp32 for every dtype.

@@ -106,7 +106,8 @@ cqsa_status move_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa
   if (empty(*K) || b->B == 0) return CQSA_OK;
   if (int64_t(b->B) * c->H > (int64_t(1) << 23))
     return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences and heads than one launch takes");
-  if (!write && K->data == V->data) return fail(CQSA_ERR_INVALID_ARG, what + "K and V are one tensor");
+  if (!write && views_share(*K, *V))
+    return fail(CQSA_ERR_INVALID_ARG, what + "K and V are one tensor, or share elements");
   if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;
   CacheMoveArgs a{};
   a.c = args_of(c, b, *K);
@@ -155,7 +156,7 @@ cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   if (causal != 0 && causal != 1) return fail(CQSA_ERR_INVALID_ARG, what + "causal must be 0 or 1");
   if (!std::isfinite(scale * kLog2e))
     return fail(CQSA_ERR_INVALID_ARG, what + "scale must be finite, in powers of two too");
-  if (!empty(*Q) && Q->data == O->data && !same_place(*Q, *O))
+  if (!empty(*Q) && !same_place(*Q, *O) && views_share(*Q, *O))
     return fail(CQSA_ERR_INVALID_ARG, what + "O overlaps Q without being Q");
   if (empty(*Q) || b->B == 0) return CQSA_OK;
   if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;

@@ -68,6 +68,54 @@ bool views_meet(const cqsa_view& x, const cqsa_view& y) {
 }
 
 namespace {
+// Whether a sum of v_t * stride_t, 0 <= v_t <= most_t, lies in [lo, hi]; the strides fall,
+// so that few v of each are near enough.
+struct Term {
+  __int128 stride, most;
+};
+bool reaches(const Term* t, int n, __int128 lo, __int128 hi, int* steps) {
+  if (hi < 0) return false;
+  if (lo <= 0) return true;
+  if (n == 0) return false;
+  if (--*steps < 0) return true;
+  __int128 rest = 0;  // the most that the terms behind this one add
+  for (int i = 1; i < n; ++i) rest += t[i].stride * t[i].most;
+  const __int128 s = t->stride;
+  const __int128 first = lo > rest ? (lo - rest + s - 1) / s : 0;
+  for (__int128 v = std::min(hi / s, t->most); v >= first; --v)
+    if (reaches(t + 1, n - 1, lo - v * s, hi - v * s, steps)) return true;
+  return false;
+}
+}  // namespace
+
+bool views_share(const cqsa_view& x, const cqsa_view& y) {
+  if (!views_meet(x, y)) return false;
+  // Rows of d elements: x's at some sum of its strides, y's counted from its last one
+  // back, so that every stride adds to their distance, which is below a row's width
+  // where two rows meet.
+  const int64_t size = elem_bytes(x.dtype);
+  Term t[6];
+  int n = 0;
+  __int128 at = __int128(reinterpret_cast<uintptr_t>(x.data)) - __int128(reinterpret_cast<uintptr_t>(y.data));
+  auto add = [&](int64_t count, int64_t stride) {
+    if (count < 2 || stride == 0) return;
+    for (int i = 0; i < n; ++i)
+      if (t[i].stride == __int128(stride) * size) {
+        t[i].most += count - 1;
+        return;
+      }
+    t[n++] = {__int128(stride) * size, count - 1};
+  };
+  add(x.B, x.stride_b), add(x.L, x.stride_l), add(x.H, x.stride_h);
+  add(y.B, y.stride_b), add(y.L, y.stride_l), add(y.H, y.stride_h);
+  at -= (extent(y) - y.d) * size;
+  std::sort(t, t + n, [](const Term& a, const Term& b) { return a.stride > b.stride; });
+  const __int128 width = x.d * size;
+  int steps = 1 << 16;
+  return reaches(t, n, 1 - width - at, width - 1 - at, &steps);
+}
+
+namespace {
 
 cqsa_status make_table(const cqsa_rotary_opts& o, cqsa_rotary_s* p) {
   if (!head_dim_ok(o.d))

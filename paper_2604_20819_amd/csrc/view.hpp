@@ -20,5 +20,8 @@ bool same_shape(const cqsa_view& x, const cqsa_view& y);
 bool same_place(const cqsa_view& x, const cqsa_view& y);
 // Whether the bytes that two views span meet.
 bool views_meet(const cqsa_view& x, const cqsa_view& y);
+// Whether two views that check_view has passed, of one dtype and d, share an element.
+// Exact, but for layouts that would take too long to tell apart, which count as sharing.
+bool views_share(const cqsa_view& x, const cqsa_view& y);
 
 }  // namespace cqsa
