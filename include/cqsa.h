@@ -430,10 +430,10 @@ void cqsa_rotary_destroy(cqsa_rotary_t* plan); /* NULL is a no-op */
  * (a cos w - b sin w, b cos w + a sin w).  inverse = 1 turns by -w: the
  * gradient of x[k] from that of y[k].  n = 1 or 2 tensors (Q, or Q and K) of
  * at most 2^20 heads together are turned in one launch; they share B, L, d and
- * the dtype.  y[k] may be x[k] itself (same data and strides); else the memory
- * that it spans must not meet what x[k] spans, nor its elements the other
- * tensor's.  pos: int32 [n_axes, B, L] in device memory,
- * any value: angles are reduced in 64-bit fixed point (2^-64 turns a position,
+ * the dtype.  y[k] may be x[k] itself (same data and strides); else it shares no
+ * element with x[k], and in any case none with the other tensor or its result
+ * (they may be parts of one buffer); this is checked.
+ * pos: int32 [n_axes, B, L] in device memory, any value: angles are reduced in 64-bit fixed point (2^-64 turns a position,
  * so 2^-33 turns at the farthest), and the products are fp32, rounded once. */
 cqsa_status cqsa_rotary(const cqsa_rotary_t* plan, const int32_t* pos, const cqsa_view* x,
                         const cqsa_view* y, int32_t n, int32_t inverse, void* hip_stream);

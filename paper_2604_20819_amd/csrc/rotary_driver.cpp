@@ -61,12 +61,6 @@ bool same_place(const cqsa_view& x, const cqsa_view& y) {
          same(x.H, x.stride_h, y.stride_h);
 }
 
-bool views_meet(const cqsa_view& x, const cqsa_view& y) {
-  if (empty(x) || empty(y)) return false;
-  const __int128 a = reinterpret_cast<uintptr_t>(x.data), b = reinterpret_cast<uintptr_t>(y.data);
-  return a < b + extent(y) * elem_bytes(y.dtype) && b < a + extent(x) * elem_bytes(x.dtype);
-}
-
 namespace {
 // Whether a sum of v_t * stride_t, 0 <= v_t <= most_t, lies in [lo, hi]; the strides fall,
 // so that few v of each are near enough.
@@ -85,6 +79,13 @@ bool reaches(const Term* t, int n, __int128 lo, __int128 hi, int* steps) {
   for (__int128 v = std::min(hi / s, t->most); v >= first; --v)
     if (reaches(t + 1, n - 1, lo - v * s, hi - v * s, steps)) return true;
   return false;
+}
+
+// Whether the bytes that two views span meet.
+bool views_meet(const cqsa_view& x, const cqsa_view& y) {
+  if (empty(x) || empty(y)) return false;
+  const __int128 a = reinterpret_cast<uintptr_t>(x.data), b = reinterpret_cast<uintptr_t>(y.data);
+  return a < b + extent(y) * elem_bytes(y.dtype) && b < a + extent(x) * elem_bytes(x.dtype);
 }
 }  // namespace
 
@@ -186,11 +187,16 @@ cqsa_status rotary_impl(const cqsa_rotary_s* p, const int32_t* pos, const cqsa_v
   for (int k = 0; k < n; ++k) {
     const bool same = empty(x[k]) || same_place(x[k], y[k]);
     in_place = in_place && same;
-    if (!same && views_meet(x[k], y[k]))
+    if (!same && views_share(x[k], y[k]))
       return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: y overlaps x without being x");
   }
-  if (n == 2 && !empty(y[0]) && y[0].data == y[1].data)
-    return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: the results are one tensor");
+  if (n == 2) {
+    if (views_share(y[0], y[1]))
+      return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: the results are one tensor, or share elements");
+    // turned in place, a result meets the other tensor where it meets the other result
+    if (!in_place && (views_share(x[0], y[1]) || views_share(x[1], y[0])))
+      return fail(CQSA_ERR_INVALID_ARG, "cqsa_rotary: a result shares elements with the other tensor");
+  }
   if (heads > (1 << 20))
     return fail(CQSA_ERR_UNSUPPORTED, "cqsa_rotary: more than 2^20 heads");
   const int64_t rows = x[0].B * x[0].L;

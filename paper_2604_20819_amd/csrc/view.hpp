@@ -18,8 +18,6 @@ cqsa_status check_view(const cqsa_view* v, const char* name, int64_t d, bool wri
 bool same_shape(const cqsa_view& x, const cqsa_view& y);
 // Whether two views of one shape have the same elements' addresses.
 bool same_place(const cqsa_view& x, const cqsa_view& y);
-// Whether the bytes that two views span meet.
-bool views_meet(const cqsa_view& x, const cqsa_view& y);
 // Whether two views that check_view has passed, of one dtype and d, share an element.
 // Exact, but for layouts that would take too long to tell apart, which count as sharing.
 bool views_share(const cqsa_view& x, const cqsa_view& y);

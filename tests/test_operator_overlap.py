@@ -19,11 +19,17 @@ def read(k, v):
     return cq.lib().cqsa_cache_read(cache(H=k.H, d=k.d), cq.cqsa_cache_batch(PTR, 5, None, None, k.B, 5, 300, 0), k, v, None)
 
 
+def rotary(xs, ys):
+    plan = cq.cqsa_rotary_plan(xs[0].d)
+    a, b = ((cq.cqsa_view * 2)(*(list(t) * 2)[:2]) for t in (xs, ys))
+    return cq.lib().cqsa_rotary(plan.handle, None, a, b, len(xs), 0, None)
+
+
 def why(status):
     """Whether the call ended at its views ("shared") or behind them ("taken")."""
     assert status == -1
     text = cq.lib().cqsa_last_error().decode()
-    if "lengths is NULL" in text:
+    if "lengths is NULL" in text or "pos is NULL" in text:
         return "taken"
     assert "overlap" in text or "one tensor" in text or "share" in text, text
     return "shared"
@@ -45,6 +51,16 @@ def test_parts_of_one_projection():
     assert why(read(part(4, 2), part(6, 2))) == "taken"
     assert why(read(part(4, 2), part(5, 2))) == "shared"
     assert why(read(part(5, 2), part(4, 2))) == "shared"
+    assert why(rotary([q], [q])) == "taken"
+    assert why(rotary([q], [part(4, 4)])) == "taken"
+    assert why(rotary([q], [part(3, 4)])) == "shared"
+    k = part(4, 2)
+    assert why(rotary([q, k], [q, k])) == "taken"
+    assert why(rotary([q, k], [part(6, 4), part(10, 2)])) == "taken"
+    assert why(rotary([q, k], [part(6, 4), part(9, 2)])) == "shared"   # the results share a head
+    assert why(rotary([q, k], [part(5, 4), part(10, 2)])) == "shared"  # q's result is on k
+    assert why(rotary([q, k], [q, part(3, 2)])) == "shared"            # k's is on q
+    assert why(rotary([k, part(6, 2)], [part(6, 2), k])) == "shared"   # swapped
 
 
 def test_heads_first_and_tokens_first():
@@ -91,5 +107,6 @@ def test_against_the_sets_of_elements(seed):
             shape, (x.stride_b, x.stride_l, x.stride_h), (y.stride_b, y.stride_l, y.stride_h)))
         want = "taken" if same or not units(x) & units(y) else "shared"
         assert why(attend(x, y)) == want
+        assert why(rotary([x], [y])) == want
         seen[want] += 1
     assert min(seen.values()) > 20
