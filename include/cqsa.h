@@ -433,8 +433,9 @@ void cqsa_rotary_destroy(cqsa_rotary_t* plan); /* NULL is a no-op */
  * the dtype.  y[k] may be x[k] itself (same data and strides); else it shares no
  * element with x[k], and in any case none with the other tensor or its result
  * (they may be parts of one buffer); this is checked.
- * pos: int32 [n_axes, B, L] in device memory, any value: angles are reduced in 64-bit fixed point (2^-64 turns a position,
- * so 2^-33 turns at the farthest), and the products are fp32, rounded once. */
+ * pos: int32 [n_axes, B, L] in device memory, any value: angles are reduced in
+ * 64-bit fixed point and are off by at most 2^-32 + 2^-64 (1 + pos_scale) |pos|
+ * turns; the products are fp32, rounded once. */
 cqsa_status cqsa_rotary(const cqsa_rotary_t* plan, const int32_t* pos, const cqsa_view* x,
                         const cqsa_view* y, int32_t n, int32_t inverse, void* hip_stream);
 

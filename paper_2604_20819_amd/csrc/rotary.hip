@@ -4,8 +4,8 @@
 // 64-bit fixed-point fraction F of a turn, so the integer product p * F modulo
 // 2^64 is the angle modulo one turn with no rounding: positions of a million
 // lose nothing, where p * f in fp32 would be off by up to 0.03 radians.  Its
-// upper 32 bits split exactly into a quarter turn and a rest within an eighth
-// turn, whose sine and cosine are their Taylor sums (x <= pi / 4: the first term
+// upper 32 bits, under 2^-32 turns less, split exactly into a quarter turn and a
+// rest within an eighth turn, whose sine and cosine are their Taylor sums (x <= pi / 4: the first term
 // left out is 2e-9 of the sine and 3e-10 of the cosine).
 #include "hip_common.hpp"
 #include "rotary.hpp"

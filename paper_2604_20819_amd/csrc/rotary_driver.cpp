@@ -153,7 +153,9 @@ cqsa_status make_table(const cqsa_rotary_opts& o, cqsa_rotary_s* p) {
     const int j = used[axis]++;
     const long double at = o.spectrum == CQSA_SPECTRUM_SHARED ? (long double)i / n
                                                               : (long double)j / o.sections[axis];
-    // radians a position, then turns without the whole ones
+    // radians a position, then turns without the whole ones: four roundings to 64 bits
+    // of a value of at most pos_scale / 2 pi turns, and that to 2^-64 turns, are under
+    // 2^-64 (1 + pos_scale) turns
     const long double f = o.pos_scale[axis] * std::pow((long double)o.theta, -at);
     long double t = f / 6.283185307179586476925286766559006L;
     t -= std::floor(t);
