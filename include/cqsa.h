@@ -480,8 +480,8 @@ uint64_t cqsa_cache_page_bytes(int32_t page_size, int32_t H, int32_t d);
  * such entries may stand for tokens that a caller has given up.
  * Values outside their range are taken as the nearest one allowed: lengths in
  * [0, max_len], q_start in [0, T] and q_start[b + 1] from q_start[b] on, n_b at most
- * max_q.  Where q_start falls, so that sequences share rows, a row of those gets
- * results of any of them. */
+ * max_q.  Where q_start falls, so that sequences share rows, what such a row (and
+ * its LSE) gets is not specified; the other rows are as without it. */
 typedef struct {
   const int32_t* pages;   /* device [B, max_pages] */
   int64_t pages_stride;   /* elements between two sequences' tables, >= max_pages */
