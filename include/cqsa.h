@@ -512,6 +512,10 @@ cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* bat
  * exponentials of the scaled scores.  A row that sees nothing gets O = 0 and LSE =
  * -infinity.  A NaN in a token reaches only rows that see it.  scale <= 0 selects
  * 1 / sqrt(d); scale log2(e) must be finite.  Scores and the softmax are fp32 for every dtype.
+ * In the product with the values a weight has 16 bits for fp16 and 24 for fp32; for bf16 it has
+ * 16, but 8, as in cqsa_forward, where a launch takes 32 rows a work group or more
+ * (cqsa_cache_attend_launch): then O is off by about 1.4 times its own rounding to bf16, and a
+ * row's bits depend on how many there are.
  * workspace: device memory of at least cqsa_cache_attend_workspace bytes, 16-byte aligned,
  * with any contents; NULL where that is 0.  Calls that may overlap, replays of captured
  * graphs among them, need workspaces of their own.
