@@ -550,15 +550,19 @@ AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa
   // 38.1, 2^17 (4096, 2048) 51.5 and 54.4, 2^18 (8192, 2048) 97.8 and 84.0; d = 192:
   // 2^15 (2048, 1024) 37.7 and 41.5, 2^16 68.3 and 51.9, 2^18 251 and 116; d = 256:
   // 2^16 68.1 and 69.9, 2^18 227 and 162.  In fp16 at d = 256 and in fp32 the
-  // queries' parts leave too few registers: fp16 takes it only for short sequences
-  // (16 of 256, 1024 rows, 119 and 66, of 1024 252 and 246, of 4096 823 and 963; split,
-  // 2^18, 257 and 317), and for fp32 it is not built (d = 128 2^20 742 and 727, d =
-  // 256 1757 and 2450).
+  // queries' parts leave too few registers: fp16 takes it only for short
+  // sequences that fill the GPU and whose rows fill its work groups to 7/8 (64 sequences of 128 tokens, 4
+  // key heads, 512 rows, 115 and 62; 64 of 256, 128 rows, 40 and 32, but 80 rows 28
+  // and 30; 32 of 512, 8 key heads, 128 rows 52 and 49, 256 rows 86 and 83; 64 of 512,
+  // 100 rows 82 and 91; 32 of 1000, 128 rows 75 and 84, 384 rows 173 and 181, 512
+  // rows 211 and 201; 16 of 1000, 512 rows 136 and 147, of 1024, 1024 rows 251 and
+  // 241; of 4096 823 and 963; split, 2^18, 257 and 317), and for fp32 it is not built
+  // (d = 128 2^20 742 and 727, d = 256 1757 and 2450).
   const int tall = attend_many_rows(dt == CQSA_F16, d);
   const int64_t row_tiles = (rows + tall - 1) / tall;
-  const bool fills = B * H * row_tiles >= 256;
+  const bool fills = B * H * row_tiles >= 256, full = 8 * rows >= 7 * tall * row_tiles;
   const bool many = dt != CQSA_F32 && rows > 64 &&
-                    (dt == CQSA_F16 && d == 256 ? fills && max_len <= 1024
+                    (dt == CQSA_F16 && d == 256 ? fills && full && max_len <= (rows >= 512 ? 1024 : 512)
                                                 : fills || units >= (d <= 128 ? 1 << 17 : 1 << 16));
   if (many) {
     p.row_groups = 0;

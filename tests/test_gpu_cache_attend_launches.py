@@ -158,3 +158,34 @@ def test_more_work_groups_than_one_dimension_takes(dtype, B, G, chunk):
         r = slice(start[b], start[b + 1])
         held(dtype, o[r], l[r], reference(case, synth.as_f64(q[:, r].contiguous())[0], b, lens[b], True), max(lens[b], 1))
     assert (o[start[-1]:] == 9).all() and (l[start[-1]:] == 9).all()
+
+
+@pytest.mark.parametrize("n,G,B,H,longest,splits", [(40, 3, 64, 4, 400, 1), (64, 4, 33, 4, 500, 1), (140, 4, 13, 4, 1000, 2)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_of_fp16_at_the_widest_head(n, G, B, H, longest, splits, causal):
+    """fp16 at d = 256 in the kernel for many rows: ends inside work groups, sequences of fewer tokens
+    than rows, of one and of none, and parts."""
+    need_gpu()
+    d = 256
+    lens = (longest, 0, 1, 70) + tuple(3 + 11 * (i % 4) for i in range(B - 4))
+    case = Case(n, lens, H, d, 32)
+    case.fill_tokens()
+    q = normal(case.g, (B, n, H * G, d), "f16")
+    most = max(longest, 1024 if splits > 1 else 0)
+    columns = np.full((B, -(-most // 32)), -1, np.int32)
+    columns[:, :case.table.shape[1]] = case.table[:, :columns.shape[1]]
+    case.table = columns
+    say("attend many f16 256", n, G, B, H, longest, causal)
+    x = launch(case, q)
+    assert (x.many, x.rows, x.splits) == (1, 128, splits)
+    run(case, q, dtype="f16", causal=causal)
+
+
+@pytest.mark.parametrize("rows,tokens,many", [(128, 512, 1), (128, 513, 0), (112, 300, 1), (111, 300, 0), (80, 200, 0),
+                                              (512, 1024, 1), (512, 1025, 0), (520, 1000, 0), (600, 1000, 1)])
+def test_when_fp16_at_the_widest_head_takes_the_kernel_for_many(rows, tokens, many):
+    need_gpu()
+    table = torch.zeros((64, 40), dtype=torch.int32, device="cuda")
+    batch = cq.CacheBatch(table, table[:, 0].contiguous(), max_len=tokens)
+    q = torch.empty((64, rows, 8, 256), dtype=torch.float16, device="cuda")
+    assert cq.cqsa_cache_attend_launch(cq.Cache4(1, 8, 256, page_size=32), batch, q).many == many
