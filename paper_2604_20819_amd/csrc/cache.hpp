@@ -66,9 +66,8 @@ struct AttendPlan {
 // rows: the most that a sequence and key head has.
 AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
 
-// Work groups of a launch of attention, with their splits: a call has at most this many
-// tiles of 16 rows, and is split only where 32 or 256 rows a work group, or a GPU that
-// they do not fill, leave as much room.
+// Tiles of 16 rows that a call may have; it is split only where they do not fill the
+// GPU, so that its work groups count in 32 bits.
 constexpr int64_t kMaxGroups = int64_t(1) << 27;
 // They lie over two dimensions of the grid, the first 2^21 wide where there is a second,
 // since one has fewer than 2^32 threads.
@@ -79,10 +78,10 @@ inline dim3 attend_grid(int64_t groups) {
 }
 
 // The kernel for many rows (of 16 bits): rows of a work group, 32 a wave, with two
-// waves on a SIMD where their registers fit (fp16 at d = 192 spills 14 of them and
-// takes 0.63 ms, with 4 waves 0.93; at d = 224 47 and 1.00 to 1.02 ms, but 0.23 to
-// 0.13 where sequences have 128 rows); tokens of a tile (64 KB of LDS for two of
-// them); launch.
+// waves on a SIMD where their registers fit or all but 13 do (bf16 at d = 256 spills
+// 13 of them and takes 0.53 ms, with 4 waves 0.81; fp16 at d = 192 13 and 0.63 ms,
+// 0.93; at d = 224 47 and 1.00 to 1.02 ms, but 0.23 to 0.13 where sequences have 128
+// rows); tokens of a tile (64 KB of LDS for two of them); launch.
 constexpr int attend_many_rows(bool f16, int d) { return f16 && d > 192 ? 128 : 256; }
 constexpr int attend_many_tokens(int d) { return d <= 128 ? 64 : 32; }
 hipError_t launch_attend_many(cqsa_dtype dt, const AttendArgs& a, const AttendPlan& p, hipStream_t s);
