@@ -55,3 +55,32 @@ def test_alike_values_come_back(dtype, d, kind, n, causal):
         assert np.array_equal(np.isneginf(got), none)
         off = np.abs(got[~none] - wl[~none])
         assert (off <= e + 2.0 ** -22 * (np.abs(wl[~none]) + 8)).all(), off.max()
+
+
+@pytest.mark.parametrize("dtype,parts", [("bf16", 2.0 ** -16), ("f16", 2.0 ** -16), ("f32", 2.0 ** -22)])
+@pytest.mark.parametrize("d", [64, 160])
+def test_values_that_cancel(dtype, parts, d):
+    """Few rows: values of both signs and weights nearly alike, so that the result is far below the
+    weights' rounding.  Bound: 2 e + parts + n 2^-23 of the weights' sum of |v| (e the scores' error) and
+    half a step, as in tests/test_gpu_cache_attend.py, with the bits that two (fp32: three) parts leave."""
+    need_gpu()
+    lens, G = (2, 3, 4, 9, 32, 33, 100, 257), 4
+    case = Case(d, lens, 1, d, 32)
+    for b, m in enumerate(lens):
+        k = case.g.standard_normal((m, 1, d))
+        v = np.where(np.arange(m) % 2, -1.0, 1.0)[:, None, None] * np.resize([1.0, 1.5, 3.0], d)
+        p, t = case.slots(b, 0, m)
+        o4.write(case.data, 32, k, v, p, t)
+    q = (torch.from_numpy(case.g.standard_normal((len(lens), 1, G, d))) / 64).to(DT[dtype])
+    say("attend cancel", dtype, d)
+    x = cq.cqsa_cache_attend_launch(case.cache(), bounded(case, "few"), q.cuda())
+    assert (x.many, x.rows) == (0, 16)
+    O = torch.full_like(q, 9.0, device="cuda")
+    cq.cqsa_cache_attend(case.cache(), bounded(case, "few"), q.cuda(), O)
+    for b, m in enumerate(lens):
+        wo, _, absv, big = reference(case, q[b].double().numpy(), b, m, True)
+        e = big * (2.0 ** -20 + d * 2.0 ** -23)
+        bound = (2 * e[..., None] + parts + m * 2.0 ** -23) * absv
+        bound = bound + torch.finfo(DT[dtype]).eps / 2 * (np.abs(wo) + bound) + (2.0 ** -25 if dtype == "f16" else 0)
+        off = np.abs(O[b].cpu().double().numpy() - wo)
+        assert (off <= bound).all(), (m, (off - bound).max())
