@@ -465,6 +465,13 @@ def _device_array(t, name, shape):
         raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
 
 
+def _int32(**sizes):
+    """Refuse sizes that a field of 32 bits would cut off."""
+    for name, x in sizes.items():
+        if not 0 <= x < 2 ** 31:
+            raise ValueError(f"{name} must be in [0, 2^31), got {x}")
+
+
 def _raw_stream():
     """The current stream of a device by its index, as an integer: torch's own short
     way where it has one (it saves 1.5 us of every call), else by its stream object."""
@@ -505,6 +512,8 @@ def cqsa_rotary_plan(d, sections=None, theta=10000.0, pairs="half", spectrum="sh
     "per_axis"; dealt: pairs dealt to the axes in turn; pos_scale: a factor of
     each axis's positions."""
     o = cqsa_rotary_opts()
+    if d >= 2 ** 31 or any(n >= 2 ** 31 for n in sections or ()):
+        raise ValueError("d and the sections must be below 2^31")
     lib().cqsa_rotary_opts_default(ctypes.byref(o), d)
     o.pairs = {"half": 0, "adjacent": 1}[pairs]
     o.spectrum = {"shared": 0, "per_axis": 1}[spectrum]
@@ -562,6 +571,7 @@ class Cache4(_Fixed):
 
     def __init__(self, n_pages, H, d, page_size=64, data=None, device="cuda"):
         torch = _torch()
+        _int32(page_size=page_size, H=H, d=d)
         per = cqsa_cache_page_bytes(page_size, H, d)
         if per == 0:
             raise ValueError("page_size must be 32, 64, 128 or 256, H in [1, 65536], "
@@ -584,6 +594,7 @@ class CacheBatch(_Fixed):
     bounds the lengths (0: the table's tokens, once a cache says how many)."""
 
     def __init__(self, pages, lengths, q_start=None, max_len=0, max_q=0):
+        _int32(max_len=max_len, max_q=max_q)
         if pages.dim() != 2 or pages.dtype != _torch().int32 or not pages.is_cuda or \
                 (pages.shape[1] > 1 and pages.stride(1) != 1):
             raise ValueError("pages must be an int32 tensor [B, max_pages] on a GPU with contiguous rows")

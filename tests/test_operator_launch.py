@@ -51,3 +51,21 @@ def test_ragged_batches_are_not_refused_by_rows_that_no_sequence_has():
         q = view(B=1, L=8192 + 1023, H=32, dtype=dtype)
         x = launch(c, b, q)
         assert x.splits * 1024 * 8 * 8192 * 4 // x.rows == most
+
+
+@pytest.mark.parametrize("kw", [dict(max_len=(1 << 32) + 300), dict(max_q=(1 << 32) + 1), dict(max_len=1 << 31), dict(max_q=-1)])
+def test_bounds_that_their_fields_do_not_hold(kw):
+    """The C structure has 32 bits: 2^32 + 300 would be a bound of 300, and tokens past it left out."""
+    with pytest.raises(ValueError, match="2\\^31"):
+        cq.CacheBatch(None, None, **kw)
+
+
+@pytest.mark.parametrize("kw", [dict(d=(1 << 32) + 64), dict(d=64, sections=((1 << 32) + 16, 16))])
+def test_rotations_that_their_fields_do_not_hold(kw):
+    with pytest.raises(ValueError, match="2\\^31"):
+        cq.cqsa_rotary_plan(**kw)
+
+
+def test_caches_that_their_fields_do_not_hold():
+    with pytest.raises(ValueError, match="2\\^31"):
+        cq.Cache4(1, (1 << 32) + 8, 64)
