@@ -61,10 +61,10 @@ __global__ void __launch_bounds__(64 * W, (few_waves(RowType<T>::kQuery, DB, NQ)
   const int b = id % c.B;
   id /= c.B;
   const int rt = id % row_tiles, sp = id / row_tiles;
-  if (sp >= splits) return;  // behind the last one, where the grid has two dimensions
   const Seq s = sequence(c, b);
   const int rows = s.n * a.G, r0 = rt * ROWS;  // at most 2^31: checked on the host
-  if (r0 >= rows) return;
+  // no such rows, or, where the grid has two dimensions, behind the last work group
+  if (r0 >= rows || sp >= splits) return;
   const int rlast = r0 + ROWS < rows ? r0 + ROWS - 1 : rows - 1;
   const int seen_min = seen_by(s, a.causal, r0 / a.G), seen_max = seen_by(s, a.causal, rlast / a.G);
   const int tiles = (seen_max + 31) >> 5;

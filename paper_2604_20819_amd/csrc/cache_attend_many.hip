@@ -52,10 +52,10 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1)
   const int b = id % c.B;
   id /= c.B;
   const int sp = id % splits, rt = row_tiles - 1 - id / splits;
-  if (rt < 0) return;  // behind the last one, where the grid has two dimensions
   const Seq s = sequence(c, b);
   const int rows = s.n * a.G, r0 = rt * ROWS;
-  if (r0 >= rows) return;
+  // no such rows, or, where the grid has two dimensions, behind the last work group
+  if (r0 >= rows || rt < 0) return;
   const int rlast = r0 + ROWS < rows ? r0 + ROWS - 1 : rows - 1;
   const int seen_max = seen_by(s, a.causal, rlast / a.G);
   const int tiles = (seen_max + TK - 1) / TK;
