@@ -543,27 +543,51 @@ AttendPlan plan_attend(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa
   int64_t tiles = (max_len + 31) / 32;
   const int64_t units = B * H * ((rows + 15) / 16) * tiles;
   // The kernel for many rows decodes a tile once for 256 rows, but walks its tiles
-  // with a barrier each, so it has to fill the GPU: unsplit, or with many tiles.
-  // us, few and many, bf16, 8 key heads: 64 sequences of 128 tokens, 512 rows, d =
-  // 128, 95 and 42, d = 256 195 and 82; 32 of 1000, 128 rows 33 and 28, d = 32 17
-  // and 18.  With splits, d = 128: 2^16 units (4096 tokens, 1024 rows) 36.0 and
-  // 38.1, 2^17 (4096, 2048) 51.5 and 54.4, 2^18 (8192, 2048) 97.8 and 84.0; d = 192:
-  // 2^15 (2048, 1024) 37.7 and 41.5, 2^16 68.3 and 51.9, 2^18 251 and 116; d = 256:
-  // 2^16 68.1 and 69.9, 2^18 227 and 162.  In fp16 at d = 256 and in fp32 the
-  // queries' parts leave too few registers: fp16 takes it only for short
-  // sequences that fill the GPU and whose rows fill its work groups to 7/8 (64 sequences of 128 tokens, 4
-  // key heads, 512 rows, 115 and 62; 64 of 256, 128 rows, 40 and 32, but 80 rows 28
-  // and 30; 32 of 512, 8 key heads, 128 rows 52 and 49, 256 rows 86 and 83; 64 of 512,
-  // 100 rows 82 and 91; 32 of 1000, 128 rows 75 and 84, 384 rows 173 and 181, 512
-  // rows 211 and 201; 16 of 1000, 512 rows 136 and 147, of 1024, 1024 rows 251 and
-  // 241; of 4096 823 and 963; split, 2^18, 257 and 317), and for fp32 it is not built
-  // (d = 128 2^20 742 and 727, d = 256 1757 and 2450).
+  // with a barrier each, so it has to fill the GPU: unsplit, or with many tiles.  us,
+  // few and many, bf16, 8 key heads: 64 sequences of 128 tokens, 512 rows, d = 128, 95
+  // and 42, d = 256 195 and 82; 32 of 1000, 128 rows, d = 128 34 and 30, d = 192 69
+  // and 43.  With splits, one sequence: d = 32 and 64, 2^17 units (4096 tokens, 2048
+  // rows) 36.7 and 33.8, 48.3 and 39.3; d = 128: 2^17 52.0 and 55.4, 53.5 and 65.7
+  // (2048, 4096), 5 / 4 of it (5120, 2048) 63.1 and 63.3, 2^18 97.0 and 87.5; d = 192:
+  // 2^15 (2048, 1024) 35.2 and 47.9, 2^16 68.3 and 53.6; d = 256: 2^16 68.1 and 69.9,
+  // 2^18 227 and 162.
+  // Unsplit, a work group that its rows fill in part takes as long as a full one, and
+  // sequences too short for that to show are the fewer the narrower the heads: 64
+  // sequences of 1000, 70 rows, d = 32 20.9 and 35.6, d = 64 29.1 and 39.7, d = 96 46.7
+  // and 53.1, d = 128 45.9 and 55.1, d = 224 97 and 87, d = 256 85 and 106; 100 rows, d =
+  // 128 58.1 and 55.8, d = 160 81 and 72; 140 rows, d = 32 30.0 and 41.3, 42.9 and 47.7,
+  // 69.8 and 64.3, 69.6 and 68.9, 157 and 107; of 300, 70 rows 13.6 and 16.6, 17.6
+  // and 18.5, 21.4 and 25.2, 24.7 and 26.2, 51 and 40; 128 rows 16.0 and 18.0, 21.9
+  // and 20.2, 34.7 and 27.3; of 128, 100 rows 13.3 and 11.3, 16.9 and 12.7, 19.7 and
+  // 17.6.  fp16, whose work groups have 128 rows at d = 224: of 1000, 140 rows 162 and
+  // 226, 100 rows 131 and 137; of 300, 140 rows 84 and 98.
+  // In fp16 at d = 256 and in fp32 the queries' parts leave too few registers: fp16
+  // takes it only for short sequences that fill the GPU and whose rows fill its work
+  // groups to 7/8 (64 sequences of 128 tokens, 4 key heads, 512 rows, 115 and 62; 64 of
+  // 256, 128 rows, 40 and 32, but 80 rows 28 and 30; 32 of 512, 8 key heads, 128 rows
+  // 52 and 49, 256 rows 86 and 83; 64 of 512, 100 rows 82 and 91; 32 of 1000, 128 rows
+  // 75 and 84, 384 rows 173 and 181, 512 rows 211 and 201; 16 of 1000, 512 rows 136 and
+  // 147, of 1024, 1024 rows 251 and 241; of 4096 823 and 963; split, 2^18, 257 and 317),
+  // and for fp32 it is not built (d = 128 2^20 742 and 727, d = 256 1757 and 2450).
   const int tall = attend_many_rows(dt == CQSA_F16, d);
   const int64_t row_tiles = (rows + tall - 1) / tall;
-  const bool fills = B * H * row_tiles >= 256, full = 8 * rows >= 7 * tall * row_tiles;
-  const bool many = dt != CQSA_F32 && rows > 64 &&
-                    (dt == CQSA_F16 && d == 256 ? fills && full && max_len <= (rows >= 512 ? 1024 : 512)
-                                                : fills || units >= (d <= 128 ? 1 << 17 : 1 << 16));
+  const bool fills = B * H * row_tiles >= 256;
+  int eighths = 0;  // of the work groups' rows that there have to be, unsplit
+  if (dt == CQSA_F16 && d >= 224)
+    eighths = d == 256 ? 7 : 6;
+  else if (d <= 64)
+    eighths = max_len > 384 ? 6 : 4;
+  else if (d == 96)
+    eighths = 4;
+  else if (max_len > 384 && (dt == CQSA_F16 || d <= 160 || d == 256))
+    eighths = 3;
+  if (max_len <= 128 && d < 256) eighths = 0;
+  bool many = dt != CQSA_F32 && rows > 64;
+  if (fills)
+    many = many && 8 * rows >= eighths * tall * row_tiles;
+  else
+    many = many && units >= (d <= 64 ? 1 << 17 : (d <= 128 ? 5 << 15 : 1 << 16));
+  if (dt == CQSA_F16 && d == 256) many = many && fills && max_len <= (rows >= 512 ? 1024 : 512);
   if (many) {
     p.row_groups = 0;
     p.row_tiles = int(row_tiles);

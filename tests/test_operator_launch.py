@@ -69,3 +69,23 @@ def test_rotations_that_their_fields_do_not_hold(kw):
 def test_caches_that_their_fields_do_not_hold():
     with pytest.raises(ValueError, match="2\\^31"):
         cq.Cache4(1, (1 << 32) + 8, 64)
+
+
+@pytest.mark.parametrize("dtype,d,rows,length,many", [
+    (cq.CQSA_BF16, 32, 70, 1000, 0), (cq.CQSA_BF16, 32, 140, 1000, 0), (cq.CQSA_BF16, 32, 256, 100, 1), (cq.CQSA_BF16, 32, 100, 128, 1),
+    (cq.CQSA_BF16, 64, 70, 300, 0), (cq.CQSA_BF16, 64, 128, 300, 1), (cq.CQSA_BF16, 64, 140, 1000, 0), (cq.CQSA_BF16, 64, 256, 1000, 1),
+    (cq.CQSA_BF16, 96, 70, 300, 0), (cq.CQSA_BF16, 96, 140, 1000, 1), (cq.CQSA_BF16, 128, 70, 1000, 0), (cq.CQSA_BF16, 128, 70, 300, 1),
+    (cq.CQSA_BF16, 160, 100, 1000, 1), (cq.CQSA_BF16, 224, 70, 1000, 1), (cq.CQSA_BF16, 256, 70, 1000, 0), (cq.CQSA_F16, 64, 70, 1000, 0),
+    (cq.CQSA_F16, 192, 70, 1000, 0), (cq.CQSA_F16, 224, 140, 300, 0), (cq.CQSA_F16, 224, 128, 1000, 1), (cq.CQSA_F32, 128, 256, 100, 0)])
+def test_rows_that_fill_a_work_group_in_part(dtype, d, rows, length, many):
+    """64 sequences and 8 key heads fill the GPU unsplit: the kernel for many rows where its work groups are
+    full enough for the length, by the times at the rule."""
+    x = launch(cache(H=8, d=d), long_batch(64, length), view(B=64, L=rows, H=8, d=d, dtype=dtype))
+    assert x.many == many and (x.splits == 1 or not many)
+
+
+@pytest.mark.parametrize("d,rows,length,many", [(64, 2048, 4096, 1), (96, 2048, 4096, 0), (128, 2048, 4096, 0), (128, 2048, 5120, 1),
+                                                (128, 2048, 8192, 1), (192, 1024, 4096, 1), (192, 1024, 2048, 0)])
+def test_units_that_a_split_call_needs(d, rows, length, many):
+    """One sequence and 8 key heads: 2^17 units of 16 rows by 32 tokens, 5 / 4 of that at d = 96 and 128."""
+    assert launch(cache(H=8, d=d), long_batch(1, length), view(B=1, L=rows, H=8, d=d)).many == many
