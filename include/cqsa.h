@@ -371,8 +371,10 @@ cqsa_status cqsa_forward_noalloc(const cqsa_plan_t* plan, const cqsa_tensor* Q,
                                  float* LSE, cqsa_mem lse_where, float scale, void* hip_stream);
 
 /* ------------------------------------------------------------------------
- * Operators around attention: rotary positions on Q and K, and a paged
- * key-value cache in 4 bits with the attention that reads it.
+ * Operators around attention: rotary positions on Q and K, a paged
+ * key-value cache in 4 bits with the attention that reads it, the tokens'
+ * weights in that attention and eviction by them, and the verification of
+ * drafted tokens.
  *
  * Their tensors are views of device memory with strides, so that Q, K and V
  * may be parts of one fused projection.  Every call is enqueued on
@@ -543,6 +545,100 @@ typedef struct {
  * call has no rows. */
 cqsa_status cqsa_cache_attend_launch(const cqsa_cache* cache, const cqsa_cache_batch* batch,
                                      const cqsa_view* Q, cqsa_attend_launch* out);
+
+/* A number for each cached token: fp32 [B, H, T] in device memory, token t of sequence b and the
+ * cache's head h at data[b * stride_b + h * stride_h + t].  Strides are in elements, 0 or more; what a
+ * call writes must not overlap. */
+typedef struct {
+  float* data;
+  int64_t B, H, T;
+  int64_t stride_b, stride_h;
+} cqsa_weights;
+
+/* The attention weights of the call's rows, summed for each cached token: with s_it the scaled score of
+ * query i (a row's query head of head h's group) and token t of sequence b, and i over those that see t,
+ *   W[b][h][t] = decay prior[b][h][t] + sum over i of exp(s_it - LSE_i),   0 <= t < lengths[b].
+ * Q, LSE (fp32 [B, H_q, L]), causal and scale as in cqsa_cache_attend, which leaves that LSE.  prior (or
+ * NULL: zeros) is read at the tokens that were there before the call's rows, t < lengths[b] - n_b; the rows'
+ * own tokens start from 0 whatever it holds.  prior may be W itself, else it lies apart from it (which is
+ * checked).  W from lengths[b] on is left as it was.  counts: int32 [B] in device memory, or NULL: the sums
+ * go over the first counts[b] rows of sequence b alone (taken into [0, n_b]), as where the other rows'
+ * drafts were rejected.  Rows whose LSE is not finite (they saw nothing, or a NaN) add nothing; tokens whose
+ * page holds nothing get nothing.  decay: in [0, 1].  Scores and sums are fp32 for every dtype; the order of
+ * a sum goes by the sizes of the call's arguments alone.
+ * T of W and prior is at least batch.max_len.  workspace as in cqsa_cache_attend, by
+ * cqsa_cache_weigh_workspace; the limits on a launch are that call's too. */
+cqsa_status cqsa_cache_weigh(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                             const cqsa_view* Q, const float* LSE, const int32_t* counts,
+                             const cqsa_weights* prior, float decay, const cqsa_weights* W,
+                             int32_t causal, float scale, void* workspace, uint64_t workspace_bytes,
+                             void* hip_stream);
+/* Host only: the workspace of such a call, by the sizes of its arguments alone.  *bytes may be 0. */
+cqsa_status cqsa_cache_weigh_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                                       const cqsa_view* Q, uint64_t* bytes);
+
+typedef struct {
+  int32_t budget; /* tokens that a sequence keeps at most, >= 1 */
+  int32_t first;  /* of them its first ones, whatever their weights, >= 0 */
+  int32_t recent; /* and its last ones, >= 0; first + recent <= budget */
+} cqsa_evict_opts;
+
+/* Keep the tokens of most weight.  Every head of a sequence keeps n = min(budget, lengths[b]) tokens: the
+ * first ones, the recent ones and of the others those of largest W (of equal ones the earliest; a NaN is below every
+ * number).  They stay in their order and become tokens 0 ... n - 1, and new_lengths[b] = n; heads keep
+ * different tokens.  Tokens whose page entry holds nothing are never kept and count for no budget (a first or recent
+ * one is simply gone).  Keys keep what was written, positions turned into them among it.
+ * to = NULL: in place; tokens and W move together within the sequence's pages, W_to is NULL, and bytes and
+ * weights behind the kept ones stay as they were.  Else the kept tokens go to the pages of to's tables
+ * (its lengths, q_start and bounds are not read), which share no page with the batch's (what such a page gets is not
+ * specified), and the kept tokens' weights to W_to, or nowhere where that is NULL; W stays.  Sequences share pages
+ * only where the pages that are written are each one sequence's.
+ * The batch's q_start and max_q are not read.  W: T at least max_len; W_to: T at least the smaller of budget
+ * and max_len, apart from W (checked).  to's tables have pages for that many tokens (checked).
+ * kept (or NULL): int32 [B, H, budget], the positions that the kept tokens had, -1 behind them.
+ * new_lengths: int32 [B], may be batch.lengths.
+ * B H is at most 2^23, and at most 2^27 tiles of 32 tokens may be kept.  workspace as in
+ * cqsa_cache_attend, by cqsa_cache_evict_workspace. */
+cqsa_status cqsa_cache_evict(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                             const cqsa_weights* W, const cqsa_evict_opts* opts,
+                             const cqsa_cache_batch* to, const cqsa_weights* W_to, int32_t* kept,
+                             int32_t* new_lengths, void* workspace, uint64_t workspace_bytes,
+                             void* hip_stream);
+/* Host only: the workspace of such a call; in_place = 1 where `to` is NULL. */
+cqsa_status cqsa_cache_evict_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                                       int32_t budget, int32_t in_place, uint64_t* bytes);
+
+/* Probabilities [B, N, V] in device memory, one after the other along V; strides in elements, 0 or more. */
+typedef struct {
+  const void* data;
+  cqsa_dtype dtype;
+  int64_t B, N, V;
+  int64_t stride_b, stride_n;
+} cqsa_probs;
+
+/* Drafted tokens against the target's probabilities.  target p: [B, K + 1, V], p[b][k] after k of sequence b's
+ * drafted tokens; draft q: [B, K, V] of the same dtype, what tokens[b][k] were drawn from, or NULL for tokens
+ * that come without (then q is 1 at the token and 0 elsewhere).  tokens: int32 [B, K]; counts: int32 [B] or
+ * NULL, how many of them each sequence has (taken into [0, K]; NULL: K); u: fp32 [B, K + 1] random numbers in
+ * [0, 1).  In turn, token x = tokens[b][k] is accepted where u[b][k] q[b][k][x] < p[b][k][x]; a token outside
+ * [0, V) is not.  With a the number accepted before the first that is not, one more token is drawn: where one
+ * was refused, from r(t) = max(0, p[b][a][t] - q[b][a][t]) (from p[b][a] where no t has any), else from r =
+ * p[b][a]: the lowest t at which r(0) + ... + r(t) exceeds u[b][K] times the sum of all, or the last with r(t) > 0
+ * where none does.  So tokens have the target's distribution.  Rows need not sum to 1.  Products and sums are in 64
+ * bits; probabilities that are negative, NaN or infinite count as 0, and a NaN among u as 0.
+ * out: int32 [B, K + 1], the accepted tokens, then the one drawn (-1 where no token has any probability), then
+ * -1.  n_out: int32 [B], a + 1: also how many of the rows [last token, drafted tokens] the sequence keeps, as
+ * cqsa_cache_weigh's counts take it.  lengths and new_lengths: int32 [B] or both NULL, may be one: lengths with
+ * all of a sequence's drafted tokens in the cache become those with the accepted ones, lengths[b] - (counts[b]
+ * - a), at least 0.  The rows that counts leave out are not read.
+ * 1 <= K <= 64, V <= 2^24, B <= 2^20.  workspace as in cqsa_cache_attend, by cqsa_draft_verify_workspace. */
+cqsa_status cqsa_draft_verify(const cqsa_probs* target, const cqsa_probs* draft,
+                              const int32_t* tokens, const int32_t* counts, const float* u,
+                              int32_t* out, int32_t* n_out, const int32_t* lengths,
+                              int32_t* new_lengths, void* workspace, uint64_t workspace_bytes,
+                              void* hip_stream);
+/* Host only: the workspace of such a call, by target's sizes alone (its data is not read). */
+cqsa_status cqsa_draft_verify_workspace(const cqsa_probs* target, uint64_t* bytes);
 
 /* Route the library's device workspace through a caller allocator (e.g. a
  * framework's caching allocator).  alloc(bytes, ctx) returns device memory or

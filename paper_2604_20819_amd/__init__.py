@@ -8,7 +8,8 @@ eager fallback.
 
 Names follow include/cqsa.h: ``cqsa_plan``, ``cqsa_forward``,
 ``cqsa_backward``, ``cqsa_set_timing``, ``cqsa_last_stats``,
-``cqsa_rotary``, ``cqsa_cache_write``, ``cqsa_cache_attend`` ...
+``cqsa_rotary``, ``cqsa_cache_write``, ``cqsa_cache_attend``, ``cqsa_cache_weigh``,
+``cqsa_cache_evict``, ``cqsa_draft_verify`` ...
 """
 import ctypes
 import os
@@ -112,6 +113,21 @@ class cqsa_attend_launch(ctypes.Structure):
                 ("splits", ctypes.c_int32)]
 
 
+class cqsa_weights(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("B", ctypes.c_int64), ("H", ctypes.c_int64), ("T", ctypes.c_int64),
+                ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class cqsa_evict_opts(ctypes.Structure):
+    _fields_ = [("budget", ctypes.c_int32), ("first", ctypes.c_int32), ("recent", ctypes.c_int32)]
+
+
+class cqsa_probs(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("B", ctypes.c_int64), ("N", ctypes.c_int64),
+                ("V", ctypes.c_int64), ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+
+
+_W, _E, _P = (ctypes.POINTER(x) for x in (cqsa_weights, cqsa_evict_opts, cqsa_probs))
 _V, _C, _CB = (ctypes.POINTER(x) for x in (cqsa_view, cqsa_cache, cqsa_cache_batch))
 
 # Every symbol include/cqsa.h declares, with its ctypes signature.
@@ -166,6 +182,16 @@ _SIGS = {
                                          ctypes.c_void_p]),
     "cqsa_cache_attend_workspace": (ctypes.c_int, [_C, _CB, _V, ctypes.POINTER(ctypes.c_uint64)]),
     "cqsa_cache_attend_launch": (ctypes.c_int, [_C, _CB, _V, ctypes.POINTER(cqsa_attend_launch)]),
+    "cqsa_cache_weigh": (ctypes.c_int, [_C, _CB, _V, ctypes.c_void_p, ctypes.c_void_p, _W, ctypes.c_float, _W,
+                                        ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_uint64,
+                                        ctypes.c_void_p]),
+    "cqsa_cache_weigh_workspace": (ctypes.c_int, [_C, _CB, _V, ctypes.POINTER(ctypes.c_uint64)]),
+    "cqsa_cache_evict": (ctypes.c_int, [_C, _CB, _W, _E, _CB, _W, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                        ctypes.c_uint64, ctypes.c_void_p]),
+    "cqsa_cache_evict_workspace": (ctypes.c_int, [_C, _CB, ctypes.c_int32, ctypes.c_int32,
+                                                  ctypes.POINTER(ctypes.c_uint64)]),
+    "cqsa_draft_verify": (ctypes.c_int, [_P, _P] + [ctypes.c_void_p] * 8 + [ctypes.c_uint64, ctypes.c_void_p]),
+    "cqsa_draft_verify_workspace": (ctypes.c_int, [_P, ctypes.POINTER(ctypes.c_uint64)]),
     "cqsa_set_allocator": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "cqsa_set_timing": (ctypes.c_int, [ctypes.c_int32]),
     "cqsa_set_tile_counting": (ctypes.c_int, [ctypes.c_int32]),
@@ -417,17 +443,19 @@ def cqsa_backward(plan, Q, K, V, O, LSE, dO, dQ, dK, dV, scale=0.0, stream=None)
 # microseconds each, so views are packed straight into cqsa_view's bytes (a
 # third of a ctypes structure's time).
 _VIEW = struct.Struct("=Qi4x7q")
+_WEIGHTS = struct.Struct("=Q5q")
+_PROBS = struct.Struct("=Qi4x5q")
 _calls = {}
 
 
 def _call(name):
-    """The library's function, with the cqsa_view arguments as bytes."""
+    """The library's function, with the cqsa_view, cqsa_weights and cqsa_probs arguments as bytes."""
     f = _calls.get(name)
     if f is None:
         res, args = _SIGS[name]
         lib()
         f = ctypes.CDLL(LIB_PATH)[name]
-        f.restype, f.argtypes = res, [ctypes.c_char_p if x is _V else x for x in args]
+        f.restype, f.argtypes = res, [ctypes.c_char_p if x in (_V, _W, _P) else x for x in args]
         _calls[name] = f
     return f
 
@@ -610,15 +638,22 @@ class CacheBatch(_Fixed):
         self.__dict__.update(pages=pages, lengths=lengths, q_start=q_start, max_len=max_len, max_q=max_q,
                              device=device, view=view)
 
-    def _of(self, cache, t):
-        """The descriptor for a cache and a tensor of rows: the bounds left open filled in."""
-        if self.max_len and (self.max_q or self.q_start is None):
+    def _bound(self, cache):
+        """The descriptor for a cache, without rows: a bound on the lengths left open filled in."""
+        if self.max_len:
             return self.view
         v = cqsa_cache_batch.from_buffer_copy(self.view)
-        if not self.max_len:
-            v.max_len = min(v.max_pages * cache.page_size, 2 ** 30)
-        if not self.max_q:
-            v.max_q = t.shape[1]
+        v.max_len = min(v.max_pages * cache.page_size, 2 ** 30)
+        return v
+
+    def _of(self, cache, t):
+        """The descriptor for a cache and a tensor of rows: the bounds left open filled in."""
+        v = self._bound(cache)
+        if self.max_q or self.q_start is None:
+            return v
+        if v is self.view:
+            v = cqsa_cache_batch.from_buffer_copy(v)
+        v.max_q = t.shape[1]
         return v
 
 
@@ -662,15 +697,31 @@ def cqsa_cache_attend_launch(cache, batch, Q):
     return out
 
 
-def _workspace_on(stream, cache, batch, Q):
-    """A workspace from torch's allocator for one call on `stream` (None: the current one)."""
+def _workspace_on(stream, device, make, *args):
+    """make(*args), a workspace from torch's allocator, for one call on `stream` (None: the current one)."""
     if stream is None:
-        return cqsa_cache_attend_workspace(cache, batch, Q)
+        return make(*args)
     cuda = _torch().cuda
     handle = getattr(stream, "value", stream) or 0
-    with cuda.stream(cuda.ExternalStream(handle, device=cache.device) if handle
-                     else cuda.default_stream(cache.device)):
-        return cqsa_cache_attend_workspace(cache, batch, Q)
+    with cuda.stream(cuda.ExternalStream(handle, device=device) if handle else cuda.default_stream(device)):
+        return make(*args)
+
+
+def _place(workspace, device):
+    """The address and size of a workspace, or (None, 0)."""
+    if workspace is None:
+        return None, 0
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"the workspace must be a contiguous tensor on {device}")
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def _lse(LSE, Q, device):
+    """The address of an LSE for the rows of Q."""
+    want = (Q.shape[0], Q.shape[2], Q.shape[1])
+    if LSE.dtype != _torch().float32 or LSE.device != device or not LSE.is_contiguous() or LSE.shape != want:
+        raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {want} on {device}")
+    return LSE.data_ptr()
 
 
 def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, workspace=None, stream=None):
@@ -679,21 +730,143 @@ def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, work
     takes one from torch's allocator for this call and its stream."""
     device = _cache_device(cache, batch)
     vq, vo = _view(Q, device), _view(O, device)
-    lse = None
-    if LSE is not None:
-        want = (Q.shape[0], Q.shape[2], Q.shape[1])
-        if LSE.dtype != _torch().float32 or LSE.device != device or not LSE.is_contiguous() or LSE.shape != want:
-            raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {want} on {device}")
-        lse = LSE.data_ptr()
-    space, size = None, 0
+    lse = None if LSE is None else _lse(LSE, Q, device)
     if workspace is None:
-        workspace = _workspace_on(stream, cache, batch, Q)
-    if workspace is not None:
-        if workspace.device != device or not workspace.is_contiguous():
-            raise ValueError(f"the workspace must be a contiguous tensor on {device}")
-        space, size = workspace.data_ptr(), workspace.nbytes
+        workspace = _workspace_on(stream, device, cqsa_cache_attend_workspace, cache, batch, Q)
+    space, size = _place(workspace, device)
     _enqueue("cqsa_cache_attend", device, stream, cache.view, batch._of(cache, Q), vq, vo, lse,
              1 if causal else 0, scale, space, size)
+
+
+# ------------------------------- cached tokens' weights, eviction, drafted tokens
+def _weights(t, name, device):
+    """The bytes of t's cqsa_weights."""
+    s, n = t.stride(), t.shape
+    if t.dtype != _torch().float32 or t.device != device or len(s) != 3 or (n[2] > 1 and s[2] != 1):
+        raise ValueError(f"{name} must be a float32 tensor [B, H, T] on {device} with contiguous tokens")
+    return _WEIGHTS.pack(t.data_ptr(), n[0], n[1], n[2], s[0], s[1])
+
+
+def _ints(t, name, shape, device):
+    """The address of an int32 array, or None."""
+    if t is None:
+        return None
+    _device_array(t, name, shape)
+    if t.device != device:
+        raise ValueError("all tensors of a call must live on one device")
+    return t.data_ptr()
+
+
+def cqsa_cache_weigh_workspace(cache, batch, Q):
+    """A workspace for cqsa_cache_weigh with arguments of these sizes (a uint8 tensor, or
+    None where none is needed); calls that may overlap need their own."""
+    n = ctypes.c_uint64()
+    device = _cache_device(cache, batch)
+    _check(_call("cqsa_cache_weigh_workspace")(cache.view, batch._of(cache, Q), _view(Q, device), n),
+           "cqsa_cache_weigh_workspace")
+    return _torch().empty(n.value, dtype=_torch().uint8, device=device) if n.value else None
+
+
+def cqsa_cache_weigh(cache, batch, Q, LSE, W, prior=None, decay=1.0, counts=None, causal=True, scale=0.0,
+                     workspace=None, stream=None):
+    """W (fp32 [B, H, T >= max_len]) at each cached token: decay times prior (None: 0, may be
+    W; the rows' own tokens start from 0) and the sum of the attention weights that the call's
+    rows Q give it, LSE (fp32 [B, Hq, L]) being what cqsa_cache_attend left for them.  counts
+    (int32 [B]): only the first counts[b] rows of sequence b."""
+    device = _cache_device(cache, batch)
+    q, w = _view(Q, device), _weights(W, "W", device)
+    old = w if prior is W else None if prior is None else _weights(prior, "prior", device)
+    lse = _lse(LSE, Q, device)
+    n = _ints(counts, "counts", (batch.view.B,), device)
+    if workspace is None:
+        workspace = _workspace_on(stream, device, cqsa_cache_weigh_workspace, cache, batch, Q)
+    space, size = _place(workspace, device)
+    _enqueue("cqsa_cache_weigh", device, stream, cache.view, batch._of(cache, Q), q, lse, n, old, decay, w,
+             1 if causal else 0, scale, space, size)
+
+
+def _tables(to, batch, device):
+    """The cqsa_cache_batch of a target's page tables."""
+    if to.dim() != 2 or to.dtype != _torch().int32 or to.device != device or (to.shape[1] > 1 and to.stride(1) != 1):
+        raise ValueError(f"to must be an int32 tensor [B, max_pages] on {device} with contiguous rows")
+    B, n = to.shape
+    if B != batch.view.B:
+        raise ValueError("to must have a table for each of the batch's sequences")
+    return cqsa_cache_batch(to.data_ptr(), to.stride(0) if B > 1 else n, None, None, B, n, 0, 0)
+
+
+def cqsa_cache_evict_workspace(cache, batch, budget, to=None):
+    """A workspace for cqsa_cache_evict with arguments of these sizes (a uint8 tensor)."""
+    n = ctypes.c_uint64()
+    _int32(budget=budget)
+    device = _cache_device(cache, batch)
+    _check(_call("cqsa_cache_evict_workspace")(cache.view, batch._bound(cache), budget, 1 if to is None else 0, n),
+           "cqsa_cache_evict_workspace")
+    return _torch().empty(n.value, dtype=_torch().uint8, device=device) if n.value else None
+
+
+def cqsa_cache_evict(cache, batch, W, new_lengths, budget, first=0, recent=0, to=None, W_to=None, kept=None,
+                     workspace=None, stream=None):
+    """Keep, for each head of each sequence, its `first` and `recent` tokens and of the others
+    those of most weight W (fp32 [B, H, T]), `budget` in all, moved together: in place, or into
+    the pages of the tables `to` (int32 [B, max_pages]) with their weights in W_to.
+    new_lengths (int32 [B], may be the batch's lengths) and kept (int32 [B, H, budget] or None: the
+    positions they had, -1 behind them) are written."""
+    device = _cache_device(cache, batch)
+    _int32(budget=budget, first=first, recent=recent)
+    w = _weights(W, "W", device)
+    w_to = None if W_to is None else _weights(W_to, "W_to", device)
+    B = batch.view.B
+    at = _ints(kept, "kept", (B, cache.H, budget), device)
+    new = _ints(new_lengths, "new_lengths", (B,), device)
+    tables = None if to is None else _tables(to, batch, device)
+    if workspace is None:
+        workspace = _workspace_on(stream, device, cqsa_cache_evict_workspace, cache, batch, budget, to)
+    space, size = _place(workspace, device)
+    _enqueue("cqsa_cache_evict", device, stream, cache.view, batch._bound(cache), w,
+             cqsa_evict_opts(budget, first, recent), tables, w_to, at, new, space, size)
+
+
+def _probs(t, name, device):
+    """The bytes of t's cqsa_probs."""
+    s, n = t.stride(), t.shape
+    code = _dtypes().get(t.dtype)
+    if code is None or t.device != device or len(s) != 3 or (n[2] > 1 and s[2] != 1):
+        raise ValueError(f"{name} must be a float32, float16 or bfloat16 tensor [B, rows, V] on {device} with "
+                         "contiguous rows")
+    return _PROBS.pack(t.data_ptr(), code, n[0], n[1], n[2], s[0], s[1])
+
+
+def cqsa_draft_verify_workspace(target, draft=None):
+    """A workspace for cqsa_draft_verify with arguments of these sizes (a uint8 tensor, or
+    None where none is needed); calls that may overlap need their own."""
+    n = ctypes.c_uint64()
+    _check(_call("cqsa_draft_verify_workspace")(_probs(target, "target", target.device), n),
+           "cqsa_draft_verify_workspace")
+    return _torch().empty(n.value, dtype=_torch().uint8, device=target.device) if n.value else None
+
+
+def cqsa_draft_verify(target, draft, tokens, u, out, n_out, counts=None, lengths=None, new_lengths=None,
+                      workspace=None, stream=None):
+    """Accept drafted tokens (int32 [B, K]) against the target's probabilities [B, K + 1, V] and
+    the draft's [B, K, V] (None: tokens that come without), by random numbers u (fp32 [B, K + 1] in
+    [0, 1)), and draw the token behind the accepted ones.  out (int32 [B, K + 1]) gets them, -1 behind, n_out
+    (int32 [B]) how many; new_lengths those of the cache without the refused ones' rows."""
+    device = target.device
+    if not target.is_cuda:
+        raise ValueError("target must live on a GPU")
+    p = _probs(target, "target", device)
+    q = None if draft is None else _probs(draft, "draft", device)
+    B, K = target.shape[0], target.shape[1] - 1
+    if u.dtype != _torch().float32 or u.device != device or not u.is_contiguous() or u.shape != (B, K + 1):
+        raise ValueError(f"u must be a contiguous float32 tensor of shape {(B, K + 1)} on {device}")
+    arrays = [_ints(t, name, shape, device) for t, name, shape in (
+        (tokens, "tokens", (B, K)), (counts, "counts", (B,)), (out, "out", (B, K + 1)), (n_out, "n_out", (B,)),
+        (lengths, "lengths", (B,)), (new_lengths, "new_lengths", (B,)))]
+    if workspace is None:
+        workspace = _workspace_on(stream, device, cqsa_draft_verify_workspace, target)
+    space, size = _place(workspace, device)
+    _enqueue("cqsa_draft_verify", device, stream, p, q, arrays[0], arrays[1], u.data_ptr(), *arrays[2:], space, size)
 
 
 def cqsa_set_timing(enable):

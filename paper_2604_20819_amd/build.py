@@ -25,10 +25,10 @@ COMMON = [
 ]
 SOURCES = [
     "plan.cpp", "capi_plan.cpp", "runtime.cpp", "fwd_driver.cpp", "bwd_driver.cpp", "guard.cpp",
-    "rotary_driver.cpp", "cache_driver.cpp",
+    "rotary_driver.cpp", "cache_driver.cpp", "verify_driver.cpp",
     "attn_fwd.hip", "merge.hip", "attn_bwd.hip", "stage.hip",
     "rotary.hip", "cache_quant.hip", "cache_attend.hip",
-    "cache_attend_many.hip",
+    "cache_attend_many.hip", "cache_weigh.hip", "cache_evict.hip", "verify.hip",
 ]
 
 

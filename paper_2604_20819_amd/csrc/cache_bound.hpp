@@ -1,0 +1,47 @@
+// Arguments of the operators that bound the 4-bit cache: the tokens' attention
+// weights and eviction by them (internal).
+#pragma once
+
+#include "cache.hpp"
+
+namespace cqsa {
+
+// fp32 [B, H, T], a number for each cached token; strides in elements.
+struct TokenWeights {
+  float* p;
+  int64_t b, h;
+};
+
+struct WeighArgs {
+  CacheArgs c;
+  CacheTensor q;
+  const float* lse;       // [B, Hq, rows]
+  const int32_t* counts;  // or null
+  TokenWeights prior, w;  // prior.p or null
+  int32_t Hq, G;
+  int32_t causal;
+  float scale_log2;
+  float decay;
+};
+
+struct EvictArgs {
+  CacheArgs c;  // the cache and the sequences as they are
+  TokenWeights w, w_to;
+  const int32_t* to_pages;  // not in place
+  int64_t to_stride;
+  bool in_place;
+  int32_t budget, first, recent;
+  int32_t cap;          // the most tokens that a sequence keeps
+  int32_t* kept;        // [B, H, kept_stride]
+  int64_t kept_stride;
+  bool pad;             // -1 behind the kept tokens' positions
+  int32_t* n_kept;      // [B], workspace
+  int32_t* new_lengths;
+  char* stage;          // in place: [B, H, ceil(cap / 32)] tiles,
+  float* stage_w;       // and [B, H, cap] weights
+};
+
+hipError_t launch_cache_weigh(cqsa_dtype dt, const WeighArgs& a, hipStream_t s);
+hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t s);
+
+}  // namespace cqsa

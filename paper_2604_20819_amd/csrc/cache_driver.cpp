@@ -1,8 +1,10 @@
 // The entry points of the 4-bit cache: argument checks and launches.
 #include "cache.hpp"
 
+#include <algorithm>
 #include <cmath>
 
+#include "cache_bound.hpp"
 #include "runtime.hpp"
 #include "view.hpp"
 
@@ -187,22 +189,208 @@ cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   return CQSA_OK;
 }
 
+Range weights_range(const char* name, const cqsa_weights* w) {
+  if (!w || w->B == 0 || w->H == 0 || w->T == 0) return {name, 0, 0};
+  const uint64_t last = uint64_t(w->B - 1) * uint64_t(w->stride_b) + uint64_t(w->H - 1) * uint64_t(w->stride_h) +
+                        uint64_t(w->T);
+  return range_of(name, w->data, last * 4);
+}
+Range cache_range(const cqsa_cache* c) {
+  return range_of("the cache", c->data, uint64_t(c->n_pages) * cqsa_cache_page_bytes(c->page_size, c->H, c->d));
+}
+
+// Shape, alignment and strides of numbers for B sequences' tokens; `written`: they must not overlap.
+cqsa_status check_weights(const cqsa_weights* w, const char* name, const cqsa_cache* c, const cqsa_cache_batch* b,
+                          int64_t tokens, bool written, const std::string& what) {
+  const std::string n = what + name;
+  if (!w) return fail(CQSA_ERR_INVALID_ARG, n + " is NULL");
+  if (w->B != b->B || w->H != c->H)
+    return fail(CQSA_ERR_INVALID_ARG, n + "'s B and H differ from the batch's and the cache's");
+  if (w->T < tokens || w->T > (int64_t(1) << 31))
+    return fail(CQSA_ERR_INVALID_ARG, n + " must have T = " + std::to_string(tokens) + " or more, below 2^31");
+  if (w->B == 0 || w->T == 0) return CQSA_OK;
+  if (!w->data || reinterpret_cast<uintptr_t>(w->data) % 4 != 0)
+    return fail(CQSA_ERR_INVALID_ARG, n + ".data is NULL or not 4-byte aligned");
+  struct Axis {
+    int64_t n, stride;
+  } ax[2] = {{w->B, w->stride_b}, {w->H, w->stride_h}};
+  for (const Axis& a : ax)
+    if (a.n > 1 && (a.stride < 0 || a.stride > (int64_t(1) << 40)))
+      return fail(CQSA_ERR_INVALID_ARG, n + "'s strides must be in [0, 2^40]");
+  if (!written) return CQSA_OK;
+  if (ax[0].stride < ax[1].stride) std::swap(ax[0], ax[1]);
+  int64_t span = w->T;  // of the tokens, then with the axis of the smaller stride too
+  for (int i = 1; i >= 0; --i) {
+    if (ax[i].n == 1) continue;
+    if (ax[i].stride < span) return fail(CQSA_ERR_INVALID_ARG, n + " is written and overlaps itself");
+    span += ax[i].stride * (ax[i].n - 1);
+  }
+  return CQSA_OK;
+}
+bool same_weights(const cqsa_weights& x, const cqsa_weights& y) {
+  return x.data == y.data && (x.B == 1 || x.stride_b == y.stride_b) && (x.H == 1 || x.stride_h == y.stride_h);
+}
+TokenWeights weights_of(const cqsa_weights* w) {
+  return w ? TokenWeights{w->data, w->stride_b, w->stride_h} : TokenWeights{nullptr, 0, 0};
+}
+
+cqsa_status check_workspace(const void* p, uint64_t bytes, uint64_t need, const std::string& what) {
+  if (need == 0) return CQSA_OK;
+  if (!p || bytes < need)
+    return fail(CQSA_ERR_INVALID_ARG, what + "the workspace has " + std::to_string(p ? bytes : 0) +
+                                          " bytes, the call needs " + std::to_string(need));
+  if (reinterpret_cast<uintptr_t>(p) % 16 != 0)
+    return fail(CQSA_ERR_INVALID_ARG, what + "the workspace must be 16-byte aligned");
+  return CQSA_OK;
+}
+
+cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view* Q, const float* LSE,
+                       const int32_t* counts, const cqsa_weights* prior, float decay, const cqsa_weights* W,
+                       int32_t causal, float scale, void* workspace, uint64_t workspace_bytes, hipStream_t s) {
+  const std::string what = "cqsa_cache_weigh: ";
+  cqsa_status st;
+  if ((st = check_attend(c, b, Q, what)) != CQSA_OK) return st;
+  if (causal != 0 && causal != 1) return fail(CQSA_ERR_INVALID_ARG, what + "causal must be 0 or 1");
+  if (!std::isfinite(scale * kLog2e))
+    return fail(CQSA_ERR_INVALID_ARG, what + "scale must be finite, in powers of two too");
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(CQSA_ERR_INVALID_ARG, what + "decay must be in [0, 1]");
+  if ((st = check_weights(W, "W", c, b, b->max_len, true, what)) != CQSA_OK) return st;
+  if (prior && (st = check_weights(prior, "prior", c, b, b->max_len, false, what)) != CQSA_OK) return st;
+  if (b->B == 0 || b->max_len == 0) return CQSA_OK;
+  if (int64_t(b->B) * c->H > (int64_t(1) << 23))
+    return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences and heads than one launch takes");
+  if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;
+  if (reinterpret_cast<uintptr_t>(counts) % 4 != 0)
+    return fail(CQSA_ERR_INVALID_ARG, what + "counts must be 4-byte aligned");
+  if (!empty(*Q) && (!LSE || reinterpret_cast<uintptr_t>(LSE) % 4 != 0))
+    return fail(CQSA_ERR_INVALID_ARG, what + "LSE is NULL or not 4-byte aligned");
+  const uint64_t need = 0;
+  if ((st = check_workspace(workspace, workspace_bytes, need, what)) != CQSA_OK) return st;
+  const Range w = weights_range("W", W);
+  const bool in_place = prior && same_weights(*prior, *W);
+  if ((st = check_apart({w}, {range_of("LSE", LSE, uint64_t(Q->B) * Q->L * Q->H * 4), cache_range(c),
+                              in_place ? Range{"", 0, 0} : weights_range("prior", prior),
+                              range_of("counts", counts, 4 * uint64_t(b->B)),
+                              range_of("the lengths", b->lengths, 4 * uint64_t(b->B))},
+                        what)) != CQSA_OK)
+    return st;
+  WeighArgs a{};
+  a.c = args_of(c, b, *Q);
+  a.q = tensor_of(*Q);
+  a.lse = LSE;
+  a.counts = counts;
+  a.prior = weights_of(prior);
+  a.w = weights_of(W);
+  a.Hq = int32_t(Q->H);
+  a.G = int32_t(Q->H / c->H);
+  a.causal = causal;
+  a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(float(c->d))) * kLog2e;
+  a.decay = decay;
+  CQSA_HIP(launch_cache_weigh(Q->dtype, a, s));
+  return CQSA_OK;
+}
+
+// Parts of an eviction's workspace, each 16-byte aligned, by the sizes of its arguments.
+struct EvictSpace {
+  int64_t cap, tiles;
+  uint64_t n_kept, kept, stage, stage_w, bytes;
+};
+EvictSpace evict_space(const cqsa_cache* c, const cqsa_cache_batch* b, int32_t budget, bool in_place) {
+  EvictSpace e{};
+  e.cap = std::min(budget, b->max_len);
+  e.tiles = (e.cap + 31) / 32;
+  const uint64_t heads = uint64_t(b->B) * uint64_t(c->H);
+  auto part = [&](uint64_t bytes) {
+    const uint64_t at = e.bytes;
+    e.bytes += (bytes + 15) / 16 * 16;
+    return at;
+  };
+  e.n_kept = part(4 * uint64_t(b->B));
+  e.kept = part(4 * heads * uint64_t(e.cap));
+  e.stage = part(in_place ? heads * uint64_t(e.tiles) * uint64_t(tile_bytes(c->d)) : 0);
+  e.stage_w = part(in_place ? 4 * heads * uint64_t(e.cap) : 0);
+  return e;
+}
+
+cqsa_status check_evict(const cqsa_cache* c, const cqsa_cache_batch* b, int32_t budget, const std::string& what) {
+  cqsa_status st;
+  if ((st = check_cache(c, what)) != CQSA_OK) return st;
+  if ((st = check_batch(c, b, what)) != CQSA_OK) return st;
+  if (budget < 1) return fail(CQSA_ERR_INVALID_ARG, what + "budget must be 1 or more");
+  const int64_t heads = int64_t(b->B) * c->H, tiles = (int64_t(std::min(budget, b->max_len)) + 31) / 32;
+  if (heads > (int64_t(1) << 23) || heads * tiles > kMaxGroups)
+    return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences, heads and tokens than one launch takes");
+  return CQSA_OK;
+}
+
+cqsa_status evict_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_weights* W,
+                       const cqsa_evict_opts* o, const cqsa_cache_batch* to, const cqsa_weights* W_to, int32_t* kept,
+                       int32_t* new_lengths, void* workspace, uint64_t workspace_bytes, hipStream_t s) {
+  const std::string what = "cqsa_cache_evict: ";
+  cqsa_status st;
+  if (!o) return fail(CQSA_ERR_INVALID_ARG, what + "opts is NULL");
+  if ((st = check_evict(c, b, o->budget, what)) != CQSA_OK) return st;
+  if (o->first < 0 || o->recent < 0 || int64_t(o->first) + o->recent > o->budget)
+    return fail(CQSA_ERR_INVALID_ARG, what + "first and recent must be 0 or more, and budget or less together");
+  const EvictSpace e = evict_space(c, b, o->budget, !to);
+  if ((st = check_weights(W, "W", c, b, b->max_len, !to, what)) != CQSA_OK) return st;
+  if (W_to) {
+    if (!to) return fail(CQSA_ERR_INVALID_ARG, what + "W_to must be NULL in place: W is moved");
+    if ((st = check_weights(W_to, "W_to", c, b, e.cap, true, what)) != CQSA_OK) return st;
+  }
+  if (to) {
+    if (to->B != b->B) return fail(CQSA_ERR_INVALID_ARG, what + "to.B differs from the batch's");
+    if (to->max_pages < 0 || to->pages_stride < to->max_pages)
+      return fail(CQSA_ERR_INVALID_ARG, what + "to.pages_stride must be to.max_pages or more, and that 0 or more");
+    if (int64_t(to->max_pages) * c->page_size < e.cap)
+      return fail(CQSA_ERR_INVALID_ARG, what + "to's tables must have pages for min(budget, max_len) tokens");
+  }
+  if (b->B == 0) return CQSA_OK;
+  if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;
+  if (to && e.cap > 0 && (!to->pages || reinterpret_cast<uintptr_t>(to->pages) % 4 != 0))
+    return fail(CQSA_ERR_INVALID_ARG, what + "to.pages is NULL or not 4-byte aligned");
+  if (!new_lengths || reinterpret_cast<uintptr_t>(new_lengths) % 4 != 0)
+    return fail(CQSA_ERR_INVALID_ARG, what + "new_lengths is NULL or not 4-byte aligned");
+  if (reinterpret_cast<uintptr_t>(kept) % 4 != 0)
+    return fail(CQSA_ERR_INVALID_ARG, what + "kept must be 4-byte aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, e.bytes, what)) != CQSA_OK) return st;
+  const uint64_t heads = uint64_t(b->B) * uint64_t(c->H), four = 4 * uint64_t(b->B);
+  const Range none{"", 0, 0}, w = weights_range("W", W);
+  if ((st = check_apart({range_of("kept", kept, 4 * heads * uint64_t(o->budget)),
+                         range_of("new_lengths", new_lengths, four), cache_range(c),
+                         range_of("the workspace", workspace, e.bytes), weights_range("W_to", W_to), to ? none : w},
+                        {to ? w : none, new_lengths == b->lengths ? none : range_of("the lengths", b->lengths, four)},
+                        what)) != CQSA_OK)
+    return st;
+  cqsa_view rows{};  // the call has none
+  EvictArgs a{};
+  a.c = args_of(c, b, rows);
+  a.w = weights_of(W);
+  a.w_to = weights_of(W_to);
+  a.to_pages = to ? to->pages : nullptr;
+  a.to_stride = to ? to->pages_stride : 0;
+  a.in_place = !to;
+  a.budget = o->budget;
+  a.first = o->first;
+  a.recent = o->recent;
+  a.cap = int32_t(e.cap);
+  char* const space = (char*)workspace;
+  a.kept = kept ? kept : (int32_t*)(space + e.kept);
+  a.kept_stride = kept ? o->budget : e.cap;
+  a.pad = kept != nullptr;
+  a.n_kept = (int32_t*)(space + e.n_kept);
+  a.new_lengths = new_lengths;
+  a.stage = space + e.stage;
+  a.stage_w = (float*)(space + e.stage_w);
+  CQSA_HIP(launch_cache_evict(a, s));
+  return CQSA_OK;
+}
+
 }  // namespace
 
 }  // namespace cqsa
 
 using namespace cqsa;
-
-// Every entry point reports an exception as a status.
-#define CQSA_ENTRY(name, expr)                                          \
-  clear_error();                                                        \
-  try {                                                                 \
-    return expr;                                                        \
-  } catch (const std::exception& e) {                                   \
-    return fail(CQSA_ERR_INTERNAL, std::string(name ": ") + e.what());  \
-  } catch (...) {                                                       \
-    return fail(CQSA_ERR_INTERNAL, name ": unknown exception");         \
-  }
 
 extern "C" {
 
@@ -262,6 +450,54 @@ static cqsa_status launch_impl(const cqsa_cache* cache, const cqsa_cache_batch* 
 cqsa_status cqsa_cache_attend_launch(const cqsa_cache* cache, const cqsa_cache_batch* batch,
                                      const cqsa_view* Q, cqsa_attend_launch* out) {
   CQSA_ENTRY("cqsa_cache_attend_launch", launch_impl(cache, batch, Q, out))
+}
+
+cqsa_status cqsa_cache_weigh(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                             const cqsa_view* Q, const float* LSE, const int32_t* counts,
+                             const cqsa_weights* prior, float decay, const cqsa_weights* W,
+                             int32_t causal, float scale, void* workspace, uint64_t workspace_bytes,
+                             void* hip_stream) {
+  CQSA_ENTRY("cqsa_cache_weigh", weigh_impl(cache, batch, Q, LSE, counts, prior, decay, W, causal, scale, workspace,
+                                            workspace_bytes, (hipStream_t)hip_stream))
+}
+
+static cqsa_status weigh_workspace_impl(const cqsa_cache* cache, const cqsa_cache_batch* batch, const cqsa_view* Q,
+                                        uint64_t* bytes) {
+  const std::string what = "cqsa_cache_weigh_workspace: ";
+  if (!bytes) return fail(CQSA_ERR_INVALID_ARG, what + "bytes is NULL");
+  *bytes = 0;
+  return check_attend(cache, batch, Q, what);
+}
+
+cqsa_status cqsa_cache_weigh_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                                       const cqsa_view* Q, uint64_t* bytes) {
+  CQSA_ENTRY("cqsa_cache_weigh_workspace", weigh_workspace_impl(cache, batch, Q, bytes))
+}
+
+cqsa_status cqsa_cache_evict(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                             const cqsa_weights* W, const cqsa_evict_opts* opts,
+                             const cqsa_cache_batch* to, const cqsa_weights* W_to, int32_t* kept,
+                             int32_t* new_lengths, void* workspace, uint64_t workspace_bytes,
+                             void* hip_stream) {
+  CQSA_ENTRY("cqsa_cache_evict", evict_impl(cache, batch, W, opts, to, W_to, kept, new_lengths, workspace,
+                                            workspace_bytes, (hipStream_t)hip_stream))
+}
+
+static cqsa_status evict_workspace_impl(const cqsa_cache* cache, const cqsa_cache_batch* batch, int32_t budget,
+                                        int32_t in_place, uint64_t* bytes) {
+  const std::string what = "cqsa_cache_evict_workspace: ";
+  if (!bytes) return fail(CQSA_ERR_INVALID_ARG, what + "bytes is NULL");
+  *bytes = 0;
+  if (in_place != 0 && in_place != 1) return fail(CQSA_ERR_INVALID_ARG, what + "in_place must be 0 or 1");
+  const cqsa_status st = check_evict(cache, batch, budget, what);
+  if (st != CQSA_OK || batch->B == 0) return st;
+  *bytes = evict_space(cache, batch, budget, in_place).bytes;
+  return CQSA_OK;
+}
+
+cqsa_status cqsa_cache_evict_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,
+                                       int32_t budget, int32_t in_place, uint64_t* bytes) {
+  CQSA_ENTRY("cqsa_cache_evict_workspace", evict_workspace_impl(cache, batch, budget, in_place, bytes))
 }
 
 }  // extern "C"

@@ -1,0 +1,24 @@
+// Verification of drafted tokens (internal).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cqsa.h"
+
+namespace cqsa {
+
+struct VerifyArgs {
+  const void *p, *q;  // q or null
+  int64_t p_b, p_n, q_b, q_n;
+  const int32_t *tokens, *counts;
+  const float* u;
+  int32_t *out, *n_out;
+  const int32_t* lengths;
+  int32_t* new_lengths;
+  int32_t B, K, V;
+};
+
+hipError_t launch_verify(cqsa_dtype dt, const VerifyArgs& a, hipStream_t s);
+
+}  // namespace cqsa

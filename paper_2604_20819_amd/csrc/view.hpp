@@ -1,6 +1,7 @@
 // Checks of strided device tensors (cqsa_view), shared by the operators.
 #pragma once
 
+#include <initializer_list>
 #include <string>
 
 #include "cqsa.h"
@@ -22,4 +23,38 @@ bool same_place(const cqsa_view& x, const cqsa_view& y);
 // Exact, but for layouts that would take too long to tell apart, which count as sharing.
 bool views_share(const cqsa_view& x, const cqsa_view& y);
 
+// The bytes that an array or a view may touch, and its name; empty where an argument is not given.
+struct Range {
+  const char* name;
+  uintptr_t lo, hi;
+};
+inline Range range_of(const char* name, const void* p, uint64_t bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return {name, at, p ? at + bytes : at};
+}
+// No range of `written` may meet another of them, or one of `read`.
+inline cqsa_status check_apart(std::initializer_list<Range> written, std::initializer_list<Range> read,
+                               const std::string& what) {
+  auto meet = [](const Range& x, const Range& y) { return x.lo < y.hi && y.lo < x.hi && x.lo < x.hi && y.lo < y.hi; };
+  for (const Range* w = written.begin(); w != written.end(); ++w) {
+    for (const Range* x = w + 1; x != written.end(); ++x)
+      if (meet(*w, *x)) return fail(CQSA_ERR_INVALID_ARG, what + w->name + " overlaps " + x->name);
+    for (const Range& x : read)
+      if (meet(*w, x)) return fail(CQSA_ERR_INVALID_ARG, what + w->name + " overlaps " + x.name);
+  }
+  return CQSA_OK;
+}
+
 }  // namespace cqsa
+
+// Every entry point reports an exception as a status.
+#define CQSA_ENTRY(name, expr)                                          \
+  clear_error();                                                        \
+  try {                                                                 \
+    return expr;                                                        \
+  } catch (const std::exception& e) {                                   \
+    return fail(CQSA_ERR_INTERNAL, std::string(name ": ") + e.what());  \
+  } catch (...) {                                                       \
+    return fail(CQSA_ERR_INTERNAL, name ": unknown exception");         \
+  }
+

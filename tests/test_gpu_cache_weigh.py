@@ -1,0 +1,256 @@
+"""cqsa_cache_weigh against the float64 oracle.
+
+The bound: a weight exp(s - LSE) is off relatively by what its exponent is off, whose fp32
+sum of d exact products and whose steps (times the scale, minus LSE, in powers of two) round at
+most d + 8 times at the size of the sum of |q k| or LSE, and by some units of the exponential; a sum of n
+positive terms adds n half steps, and W one.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_20819_amd as cq
+from oracle import bounded as ob
+from oracle import cache4 as o4
+from tests.gpu_util import need_gpu, say
+from tests.op_util import DT, Case, normal, starts
+
+pytestmark = pytest.mark.gpu
+HALF = 2.0 ** -24
+
+
+def attended(case, cache, batch, q, causal, scale=0.0):
+    lse = torch.full((q.shape[0], q.shape[2], q.shape[1]), math.nan, device="cuda")
+    cq.cqsa_cache_attend(cache, batch, q, torch.empty_like(q), lse, causal=causal, scale=scale)
+    return lse
+
+
+def check(case, q, lse, W, new, counts, causal, scale, prior, decay, packed, first=0, untouched=None):
+    """Every sequence's weights against the oracle; what lies behind its tokens is untouched."""
+    torch.cuda.synchronize()
+    d, G = case.d, q.shape[2] // case.H
+    Wc, lc, qc = W.cpu().double().numpy(), lse.cpu().double().numpy(), q.cpu().double().numpy()
+    at, worst = first, 0.0
+    for b, (n, m) in enumerate(zip(case.lens, new)):
+        rows = slice(at, at + m) if packed else slice(0, m)
+        bb = 0 if packed else b
+        page, tok = case.slots(b, 0, n)
+        k, _ = o4.read(case.data, case.page, case.H, d, page, tok)
+        there = (page >= 0) & (page < case.n_pages)
+        old = None if prior is None else prior[b].cpu().double().numpy()
+        c = m if counts is None else min(max(int(counts[b]), 0), m)
+        want, big = ob.weigh(qc[bb, rows], k, lc[bb][:, rows].T, there, n, c, causal, scale, old, decay)
+        got = Wc[b, :, :n]
+        bound = want * HALF * ((d + 8) * big + c * G + 16) + 1e-36
+        err = np.abs(got - want)
+        assert np.isfinite(got).all() and (err <= bound).all(), (b, err.max(), (err / bound).max())
+        worst = max(worst, (err / bound).max() if err.size else 0.0)
+        assert (Wc[b, :, n:] == (7.0 if untouched is None else untouched)).all()
+        at += m
+    return worst
+
+
+def run(case, Hq, new, dtype, causal=True, counts=None, decay=1.0, with_prior=True, packed=False, scale=0.0,
+        max_len=0, first=0, spare=3, in_place=False):
+    g = case.g
+    T = case.table.shape[1] * case.page + spare
+    shape = (1, first + sum(new) + 2, Hq, case.d) if packed else (len(new), new[0], Hq, case.d)
+    q = normal(g, shape, dtype).cuda()
+    cache = case.cache()
+    batch = case.batch(q_start=starts(new, first) if packed else None, max_len=max_len, max_q=max(max(new), 1) if packed else 0)
+    lse = attended(case, cache, batch, q, causal, scale)
+    prior = torch.from_numpy(g.random((len(new), case.H, T), dtype=np.float32)).cuda() if with_prior else None
+    if prior is not None:  # what the rows' own tokens and those behind hold is not read
+        for b, (n, m) in enumerate(zip(case.lens, new)):
+            prior[b, :, max(0, n - m):] = math.nan
+    W = torch.full((len(new), case.H, T), 7.0, device="cuda")
+    keep = prior
+    if in_place:
+        keep = prior.clone()
+        for b, n in enumerate(case.lens):
+            prior[b, :, n:] = 7.0
+        W = prior
+    cnt = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+    cq.cqsa_cache_weigh(cache, batch, q, lse, W, prior=prior, decay=decay, counts=cnt, causal=causal, scale=scale)
+    return check(case, q, lse, W, new, counts, causal, scale or 1 / math.sqrt(case.d), keep, decay, packed, first)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_step(d, dtype):
+    need_gpu()
+    say("weigh step", d, dtype)
+    case = Case(d, [131, 1, 0, 64, 33], 2, d, 64)
+    case.fill_tokens()
+    run(case, 6, [1] * 5, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [32, 96, 128, 224, 256])
+@pytest.mark.parametrize("n,G", [(17, 1), (40, 4), (9, 8)])
+def test_chunk(d, dtype, n, G):
+    """More rows than a tile's, causal, beginning before position 0 in the shorter sequences."""
+    need_gpu()
+    say("weigh chunk", d, dtype, n, G)
+    case = Case(d + n, [150, 20, 5], 2, d, 32)
+    case.fill_tokens()
+    run(case, 2 * G, [n] * 3, dtype, decay=0.75)
+
+
+@pytest.mark.parametrize("page", [32, 64, 128, 256])
+@pytest.mark.parametrize("causal", [True, False])
+def test_pages_and_masks(page, causal):
+    need_gpu()
+    say("weigh pages", page, causal)
+    case = Case(page, [300, 257, 31, 2], 3, 64, page)
+    case.fill_tokens()
+    run(case, 3, [4] * 4, "bf16", causal=causal, scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_packed_rows(dtype):
+    """Packed rows between rows that no sequence has, some sequences without rows."""
+    need_gpu()
+    say("weigh packed", dtype)
+    case = Case(5, [70, 40, 90, 3, 0], 2, 96, 32)
+    case.fill_tokens()
+    run(case, 4, [7, 0, 33, 5, 2], dtype, packed=True, first=3, decay=0.5)
+
+
+def test_counts():
+    need_gpu()
+    say("weigh counts")
+    case = Case(6, [50, 40, 45, 60, 33], 2, 64, 32)
+    case.fill_tokens()
+    run(case, 4, [6] * 5, "f16", counts=[6, 0, 3, 99, -4])
+
+
+def test_in_place_and_without_prior():
+    need_gpu()
+    say("weigh in place")
+    case = Case(7, [90, 33], 2, 128, 64)
+    case.fill_tokens()
+    run(case, 4, [3, 3], "bf16", decay=0.9, in_place=True)
+    run(case, 4, [3, 3], "bf16", with_prior=False, decay=0.9)
+    run(case, 4, [3, 3], "bf16", decay=0.0)
+
+
+def test_pages_that_hold_nothing():
+    need_gpu()
+    say("weigh holes")
+    case = Case(8, [200, 100], 2, 64, 32)
+    case.fill_tokens()
+    case.table[0, 2] = -1
+    case.table[0, 4] = 10 ** 6
+    case.table[1, 0] = -7
+    run(case, 2, [2, 2], "bf16")
+
+
+def test_nan_tokens_and_rows():
+    """A NaN token makes the rows that see it add nothing; the other rows' sums are as without it."""
+    need_gpu()
+    say("weigh nan")
+    case = Case(9, [64], 1, 64, 32)
+    case.fill_tokens()
+    page, tok = case.slots(0, 61, 1)
+    k = np.full((1, 1, 64), np.nan)
+    o4.write(case.data, 32, k, k, page, tok)
+    g = case.g
+    q = normal(g, (1, 8, 2, 64), "bf16").cuda()
+    q[0, 1, 0, 5] = math.nan
+    cache, batch = case.cache(), case.batch()
+    lse = attended(case, cache, batch, q, True)
+    assert torch.isnan(lse[0, :, 5:]).all() and torch.isnan(lse[0, 0, 1])
+    W = torch.zeros(1, 1, 96, device="cuda")
+    cq.cqsa_cache_weigh(cache, batch, q, lse, W)
+    q = torch.nan_to_num(q)
+    rows = lse.clone()
+    torch.cuda.synchronize()
+    k, _ = o4.read(case.data, 32, 1, 64, *case.slots(0, 0, 64))
+    want, big = ob.weigh(q.cpu().double().numpy()[0], np.nan_to_num(k), rows.cpu().double().numpy()[0].T,
+                         np.ones(64, bool), 64, 8, True, 1 / 8.0, None, 1.0)
+    got = W.cpu().double().numpy()[0, :, :64]
+    assert (np.abs(got - want) <= want * HALF * (72 * big + 32) + 1e-36).all()
+    assert got[0, 61] == 0
+
+
+def test_infinite_lse():
+    need_gpu()
+    say("weigh infinite lse")
+    case = Case(10, [40], 1, 32, 32)
+    case.fill_tokens()
+    q = normal(case.g, (1, 3, 1, 32), "bf16").cuda()
+    lse = torch.tensor([[[-math.inf, math.inf, math.nan]]], device="cuda")
+    W = torch.full((1, 1, 96), 5.0, device="cuda")
+    cq.cqsa_cache_weigh(case.cache(), case.batch(), q, lse, W)
+    assert (W[0, 0, :40] == 0).all() and (W[0, 0, 40:] == 5).all()
+
+
+def test_sums_are_the_rows():
+    """The weights of one row's tokens sum to 1, over many splits of a long context too."""
+    need_gpu()
+    say("weigh sums")
+    for B, n, L in ((1, 70001, 1), (2, 5003, 3), (1, 2500, 700)):
+        case = Case(n, [n] * B, 2, 64, 256)
+        case.data = case.g.integers(0, 256, case.data.shape, dtype=np.uint8)
+        tiles = case.data.reshape(case.n_pages, -1, 34 * 64)
+        tiles[..., 32 * 64:] = 125 + tiles[..., 32 * 64:] % 3
+        q = normal(case.g, (B, L, 4, 64), "bf16").cuda()
+        cache, batch = case.cache(), case.batch()
+        lse = attended(case, cache, batch, q, False)
+        W = torch.zeros(B, 2, case.table.shape[1] * 256, device="cuda")
+        cq.cqsa_cache_weigh(cache, batch, q, lse, W, causal=False)
+        # the errors of LSE and of the weights, 64 products' and 2^10 units at most
+        assert torch.allclose(W.double().sum(-1), torch.full((B, 2), 2.0 * L, dtype=torch.float64, device="cuda"), rtol=1e-4)
+
+
+def test_strided_tensors_and_another_stream():
+    need_gpu()
+    say("weigh strides")
+    case = Case(11, [77, 50], 2, 64, 32)
+    case.fill_tokens()
+    both = normal(case.g, (2, 3, 9, 64), "bf16").cuda()
+    q = both[:, :, 3:7]
+    store = torch.full((2, 5, 200), 7.0, device="cuda")
+    W = store[:, 1:3, 10:170]
+    cache, batch = case.cache(), case.batch()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        lse = attended(case, cache, batch, q, True)
+        cq.cqsa_cache_weigh(cache, batch, q, lse, W)
+    torch.cuda.current_stream().wait_stream(side)
+    check(case, q, lse, W, [3, 3], None, True, 0.125, None, 1.0, False)
+    store[:, 1:3, 10:170] = 7.0
+    assert (store == 7).all()
+
+
+def test_same_bits_again_and_captured():
+    """Two calls give the same bits, and so does every replay of a captured one."""
+    need_gpu()
+    say("weigh captured")
+    for lens, L in (([3000, 100], 1), ([900], 300)):
+        case = Case(12, lens, 2, 128, 64)
+        case.fill_tokens()
+        q = normal(case.g, (len(lens), L, 8, 128), "bf16").cuda()
+        cache, batch = case.cache(), case.batch()
+        lse = attended(case, cache, batch, q, True)
+        prior = torch.rand(len(lens), 2, case.table.shape[1] * 64, device="cuda")
+        W = torch.zeros_like(prior)
+        space = cq.cqsa_cache_weigh_workspace(cache, batch, q)
+        call = lambda: cq.cqsa_cache_weigh(cache, batch, q, lse, W, prior=prior, decay=0.5, workspace=space)
+        call()
+        first = W.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        for i in range(4):
+            W.fill_(float(i))
+            if space is not None:
+                space.fill_(255 - i)
+            graph.replay()
+            torch.cuda.synchronize()
+            for b, n in enumerate(lens):
+                assert torch.equal(W[b, :, :n], first[b, :, :n])
