@@ -22,7 +22,19 @@ struct WeighArgs {
   int32_t causal;
   float scale_log2;
   float decay;
+  float* part;  // with splits: [splits][B][H][max_len]
 };
+
+// How a call's rows and tokens are spread over work groups; by its sizes alone.
+struct WeighPlan {
+  bool many;       // the kernel for many rows
+  int row_groups;  // else groups of 16 rows
+  int tiles;       // work groups over a sequence's tokens
+  int splits;      // and, with many rows, over its rows
+  int64_t groups;  // work groups in all
+};
+// rows: the most that a sequence and key head has.
+WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
 
 struct EvictArgs {
   CacheArgs c;  // the cache and the sequences as they are
@@ -41,7 +53,7 @@ struct EvictArgs {
   float* stage_w;       // and [B, H, cap] weights
 };
 
-hipError_t launch_cache_weigh(cqsa_dtype dt, const WeighArgs& a, hipStream_t s);
+hipError_t launch_cache_weigh(cqsa_dtype dt, const WeighArgs& a, const WeighPlan& p, hipStream_t s);
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t s);
 
 }  // namespace cqsa

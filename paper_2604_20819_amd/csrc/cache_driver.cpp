@@ -244,12 +244,29 @@ cqsa_status check_workspace(const void* p, uint64_t bytes, uint64_t need, const 
   return CQSA_OK;
 }
 
+// The launch of a call whose arguments check_attend has passed, and its workspace.
+WeighPlan weigh_plan(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view& Q) {
+  const int64_t n = empty(Q) ? 0 : b->q_start ? b->max_q : Q.L;
+  return plan_weigh(b->B, c->H, n * (Q.H / c->H), b->max_len, Q.dtype, c->d);
+}
+uint64_t weigh_bytes(const WeighPlan& p, const cqsa_cache* c, const cqsa_cache_batch* b) {
+  return p.splits == 1 ? 0 : uint64_t(p.splits) * uint64_t(b->B) * uint64_t(c->H) * uint64_t(b->max_len) * 4;
+}
+cqsa_status check_weigh(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view* Q, const std::string& what) {
+  const cqsa_status st = check_attend(c, b, Q, what);
+  if (st != CQSA_OK) return st;
+  const int64_t heads = int64_t(b->B) * c->H, tiles = (int64_t(b->max_len) + 255) / 256;
+  if (heads > (int64_t(1) << 23) || heads * tiles > (int64_t(1) << 22) * 4)
+    return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences, heads and tokens than one launch takes");
+  return CQSA_OK;
+}
+
 cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view* Q, const float* LSE,
                        const int32_t* counts, const cqsa_weights* prior, float decay, const cqsa_weights* W,
                        int32_t causal, float scale, void* workspace, uint64_t workspace_bytes, hipStream_t s) {
   const std::string what = "cqsa_cache_weigh: ";
   cqsa_status st;
-  if ((st = check_attend(c, b, Q, what)) != CQSA_OK) return st;
+  if ((st = check_weigh(c, b, Q, what)) != CQSA_OK) return st;
   if (causal != 0 && causal != 1) return fail(CQSA_ERR_INVALID_ARG, what + "causal must be 0 or 1");
   if (!std::isfinite(scale * kLog2e))
     return fail(CQSA_ERR_INVALID_ARG, what + "scale must be finite, in powers of two too");
@@ -257,18 +274,17 @@ cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqs
   if ((st = check_weights(W, "W", c, b, b->max_len, true, what)) != CQSA_OK) return st;
   if (prior && (st = check_weights(prior, "prior", c, b, b->max_len, false, what)) != CQSA_OK) return st;
   if (b->B == 0 || b->max_len == 0) return CQSA_OK;
-  if (int64_t(b->B) * c->H > (int64_t(1) << 23))
-    return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences and heads than one launch takes");
   if ((st = check_pointers(c, b, what)) != CQSA_OK) return st;
   if (reinterpret_cast<uintptr_t>(counts) % 4 != 0)
     return fail(CQSA_ERR_INVALID_ARG, what + "counts must be 4-byte aligned");
   if (!empty(*Q) && (!LSE || reinterpret_cast<uintptr_t>(LSE) % 4 != 0))
     return fail(CQSA_ERR_INVALID_ARG, what + "LSE is NULL or not 4-byte aligned");
-  const uint64_t need = 0;
+  const WeighPlan p = weigh_plan(c, b, *Q);
+  const uint64_t need = weigh_bytes(p, c, b);
   if ((st = check_workspace(workspace, workspace_bytes, need, what)) != CQSA_OK) return st;
   const Range w = weights_range("W", W);
   const bool in_place = prior && same_weights(*prior, *W);
-  if ((st = check_apart({w}, {range_of("LSE", LSE, uint64_t(Q->B) * Q->L * Q->H * 4), cache_range(c),
+  if ((st = check_apart({w, range_of("the workspace", workspace, need)}, {range_of("LSE", LSE, uint64_t(Q->B) * Q->L * Q->H * 4), cache_range(c),
                               in_place ? Range{"", 0, 0} : weights_range("prior", prior),
                               range_of("counts", counts, 4 * uint64_t(b->B)),
                               range_of("the lengths", b->lengths, 4 * uint64_t(b->B))},
@@ -286,7 +302,8 @@ cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqs
   a.causal = causal;
   a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(float(c->d))) * kLog2e;
   a.decay = decay;
-  CQSA_HIP(launch_cache_weigh(Q->dtype, a, s));
+  a.part = (float*)workspace;
+  CQSA_HIP(launch_cache_weigh(Q->dtype, a, p, s));
   return CQSA_OK;
 }
 
@@ -466,7 +483,10 @@ static cqsa_status weigh_workspace_impl(const cqsa_cache* cache, const cqsa_cach
   const std::string what = "cqsa_cache_weigh_workspace: ";
   if (!bytes) return fail(CQSA_ERR_INVALID_ARG, what + "bytes is NULL");
   *bytes = 0;
-  return check_attend(cache, batch, Q, what);
+  const cqsa_status st = check_weigh(cache, batch, Q, what);
+  if (st != CQSA_OK || batch->B == 0 || batch->max_len == 0) return st;
+  *bytes = weigh_bytes(weigh_plan(cache, batch, *Q), cache, batch);
+  return CQSA_OK;
 }
 
 cqsa_status cqsa_cache_weigh_workspace(const cqsa_cache* cache, const cqsa_cache_batch* batch,

@@ -2,20 +2,56 @@
 // cache (gfx950): W[t] = decay prior[t] + sum over rows of exp(s_t - LSE).
 //
 // A key head's G query heads of a sequence's n tokens are n G rows of one matrix
-// product with its keys; a wave holds 32 tokens' keys and goes through the rows.
-// The product's columns are the tokens, so that a lane sums over the rows what it
-// holds and four lanes' sums make a token's.
+// product with its keys, whose columns are the tokens: a lane sums over the rows
+// what it holds of its token, with no maximum to keep, since LSE is known, and
+// the lanes of a column are added at the end.
+#include <algorithm>
+
 #include "cache_attend.hpp"
 #include "cache_bound.hpp"
 
 namespace cqsa {
 
 namespace {
+
 constexpr float kLog2eF = 1.4426950408889634f;
+
+// Rows of sequence s that count.
+__device__ __forceinline__ int rows_of(const WeighArgs& a, const Seq& s, int b) {
+  int n = a.counts ? a.counts[b] : s.n;
+  n = n < 0 ? 0 : (n > s.n ? s.n : n);
+  return n * a.G;
 }
 
-template <typename T, int DB>
-__global__ void __launch_bounds__(256) cache_weigh_rows(const WeighArgs a, int per_seq) {
+// What row `tok` of head g is shifted by, in powers of two, and the tokens that it
+// sees: none where its LSE is not finite.
+struct RowShift {
+  float shift;
+  int seen;
+};
+__device__ __forceinline__ RowShift row_shift(const WeighArgs& a, const Seq& s, int64_t tb, int h, int tok, int g) {
+  const float lse = a.lse[(tb * a.Hq + h * a.G + g) * int64_t(a.c.rows) + s.row0 + tok];
+  const bool ok = __builtin_fabsf(lse) < INFINITY;
+  return {ok ? lse * kLog2eF : INFINITY, ok ? seen_by(s, a.causal, tok) : 0};
+}
+constexpr RowShift kBlindRow = {INFINITY, 0};
+
+// Groups of 16 rows that the kernel for few rows takes in registers.
+constexpr int weigh_few_groups(int parts, int db) { return parts * db <= 8 ? 2 : 1; }
+// Waves a SIMD is to hold: as many as the registers allow without spilling.
+constexpr int weigh_few_waves(int parts, int db, int nq) {
+  const int held = parts * db * nq;
+  if (nq == 1) return held <= 18 ? 4 : held <= 21 ? 3 : 2;
+  return held <= 7 || (held == 8 && parts == 1) ? 4 : held <= 14 ? 3 : 2;
+}
+
+}  // namespace
+
+// Few rows, 16 NQ at most: they stay in registers while a wave goes through the
+// tokens in tiles of 32, the next tile's keys on their way.
+template <typename T, int DB, int NQ>
+__global__ void __launch_bounds__(256, (weigh_few_waves(RowType<T>::kQuery, DB, NQ))) cache_weigh_few(const WeighArgs a, int per_seq) {
+  constexpr bool WIDE = DB % 4 == 0;  // whole blocks a lane
   constexpr int D = 32 * DB, QP = RowType<T>::kQuery;
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
@@ -25,86 +61,370 @@ __global__ void __launch_bounds__(256) cache_weigh_rows(const WeighArgs a, int p
   id /= c.H;
   const int b = id % c.B, part = id / c.B;
   const Seq s = sequence(c, b);
-  int count = a.counts ? a.counts[b] : s.n;
-  count = count < 0 ? 0 : (count > s.n ? s.n : count);
-  const int rows = count * a.G;
-  const int old = s.len - s.n;  // tokens that were there before the rows
+  const int t1 = (s.len + 31) >> 5, step = 4 * per_seq;
+  int t = 4 * part + wave;
+  if (t >= t1) return;
+  const int rows = rows_of(a, s, b), old = s.len - s.n;
   const int64_t tb = c.q_start ? 0 : b;
   const float* prior = a.prior.p ? a.prior.p + b * a.prior.b + h * a.prior.h : nullptr;
   float* out = a.w.p + b * a.w.b + h * a.w.h;
 
-  for (int t = part * 4 + wave; 32 * t < s.len; t += 4 * per_seq) {
-    const int64_t page = page_of(c, b, t);
-    float sum[2] = {0.f, 0.f};
+  uint32_t xk[DB][2], xke[WIDE ? DB / 4 : DB];
+  float before = 0.f;
+  // lanes 0 .. 15 and 32 .. 47 hold a tile's sums in the end
+  const int mine = 16 * (quarter >> 1) + col;
+  auto load = [&](int u, int32_t page) {
     if (page >= 0) {
-      const char* p = c.data + tile_at(c, page, h, t);
-      bf16x8 kk[DB][2];
+      const char* p = c.data + tile_at(c, page, h, u);
+      if constexpr (WIDE) {
 #pragma unroll
-      for (int w = 0; w < DB; ++w) {
-        const uint32_t e = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * w);
+        for (int j = 0; j < DB / 4; ++j) {
+          const int blk = 4 * j + quarter;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-          kk[w][u] = decode8(*(const uint32_t*)(p + w * 512 + (16 * u + col) * 16 + 4 * quarter), scale_of(e, u));
-      }
-      for (int r0 = 0; r0 < rows; r0 += 16) {
-        const int r = r0 + col;
-        const T* q = (const T*)a.q.p + tb * a.q.b + int64_t(s.row0 + r / a.G) * a.q.l +
-                     int64_t(h * a.G + r % a.G) * a.q.h + 8 * quarter;
-        f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+          for (int v = 0; v < 2; ++v) {
+            const u32x4 x = *(const u32x4*)(p + blk * 512 + (16 * v + col) * 16);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) xk[4 * j + w][v] = x[w];
+          }
+          xke[j] = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * blk);
+        }
+      } else {
 #pragma unroll
         for (int w = 0; w < DB; ++w) {
-          float v[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = 0.f;
-          if (r < rows) load_row8<T>(q + 32 * w, v);
-          bf16x8 qq[QP];
-          split8<QP>(v, qq);
-#pragma unroll
-          for (int k = QP - 1; k >= 0; --k) {
-            x[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qq[k], kk[w][0], x[0], 0, 0, 0);
-            x[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qq[k], kk[w][1], x[1], 0, 0, 0);
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = r0 + 4 * quarter + e;
-          float lse = INFINITY;
-          int seen = 0;
-          if (row < rows) {
-            lse = a.lse[(tb * a.Hq + h * a.G + row % a.G) * int64_t(c.rows) + s.row0 + row / a.G];
-            if (__builtin_fabsf(lse) < INFINITY) seen = seen_by(s, a.causal, row / a.G);
-          }
-          const float shift = lse * kLog2eF;
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float y = fast_exp2(__builtin_fmaf(x[u][e], a.scale_log2, -shift));
-            sum[u] += 32 * t + 16 * u + col < seen ? y : 0.f;
-          }
+          for (int v = 0; v < 2; ++v) xk[w][v] = *(const uint32_t*)(p + w * 512 + (16 * v + col) * 16 + 4 * quarter);
+          xke[w] = *(const uint16_t*)(p + 32 * D + col * 2 * DB + 2 * w);
         }
       }
     }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float y = sum_of_quarters(sum[u]);
-      const int tok = 32 * t + 16 * u + col;
-      if (quarter == 0 && tok < s.len) out[tok] = prior && tok < old ? __builtin_fmaf(a.decay, prior[tok], y) : y;
+    const int tok = 32 * u + mine;
+    before = prior && tok < old ? prior[tok] : 0.f;
+  };
+  // pages of the wave's next 64 tiles, one a lane
+  int32_t pages = -1;
+  int at = 64;
+  auto next_page = [&](int u) {
+    if (u >= t1) return -1;
+    if (at == 64) {
+      const int v = u + step * lane;
+      pages = v < t1 ? int32_t(page_of(c, b, v)) : -1;
+      at = 0;
     }
+    return __builtin_amdgcn_readlane(pages, at++);
+  };
+  int32_t page = next_page(t);
+  load(t, page);
+
+  // Row 4 e + q of a group is the product's row 4 q + e: few rows are then few of
+  // every lane's four.
+  bf16x8 qf[NQ][DB][QP];
+  float shift[NQ][4];
+  int seen[NQ][4];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = 16 * n + 4 * (col & 3) + (col >> 2);
+    const int tok = r / a.G, g = r % a.G;
+#pragma unroll
+    for (int w = 0; w < DB; ++w) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+      const int e = WIDE ? 32 * (4 * (w / 4) + quarter) + 8 * (w % 4) : 32 * w + 8 * quarter;
+      if (r < rows)
+        load_row8<T>((const T*)a.q.p + tb * a.q.b + int64_t(s.row0 + tok) * a.q.l + int64_t(h * a.G + g) * a.q.h + e, v);
+      split8<QP>(v, qf[n][w]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 16 * n + 4 * e + quarter;
+      const RowShift x = i < rows ? row_shift(a, s, tb, h, i / a.G, i % a.G) : kBlindRow;
+      shift[n][e] = x.shift, seen[n][e] = x.seen;
+    }
+  }
+
+  while (t < t1) {
+    const int next = t + step;
+    const int32_t page2 = next_page(next);
+    const bool here = page >= 0;
+    f32x4 x[NQ][2];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) x[n][0] = x[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (here) {
+#pragma unroll
+      for (int w = 0; w < DB; ++w)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const bf16x8 kk = decode8(xk[w][v], scale_of(xke[WIDE ? w / 4 : w], v));
+#pragma unroll
+          for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int k = QP - 1; k >= 0; --k)
+              x[n][v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[n][w][k], kk, x[n][v], 0, 0, 0);
+        }
+    }
+    const float had = before;
+    if (next < t1) load(next, page2);
+    float sum[2] = {0.f, 0.f};
+    if (here) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (16 * n + 4 * e < rows) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              const float y = fast_exp2(__builtin_fmaf(x[n][v][e], a.scale_log2, -shift[n][e]));
+              sum[v] += 32 * t + 16 * v + col < seen[n][e] ? y : 0.f;
+            }
+          }
+    }
+    // the halves' lanes exchange: the lower half gets the first 16 tokens' sums
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, sum[0]),
+                                                    __builtin_bit_cast(uint32_t, sum[1]), false, false);
+    const uint32_t lo = r[0], hi = r[1];
+    float y = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+    y += __shfl_xor(y, 16);
+    const int tok = 32 * t + mine;
+    if ((quarter & 1) == 0 && tok < s.len) out[tok] = __builtin_fmaf(a.decay, had, y);
+    t = next, page = page2;
+  }
+}
+
+// Many rows: a wave keeps 64 tokens' decoded keys in registers, and the work
+// group's waves go through the rows together, stage by stage of RS through LDS,
+// where a matrix operand lies as the 64 lanes read it.
+template <typename T, int DB, int W, int RS>
+__global__ void __launch_bounds__(64 * W, 2) cache_weigh_many(const WeighArgs a, int token_tiles, int splits) {
+  constexpr int D = 32 * DB, QP = RowType<T>::kQuery, NT = 64 * W, TOKENS = 64 * W;
+  constexpr int UNITS = RS * 4 * DB, NU = (UNITS + NT - 1) / NT;  // of 8 elements
+  __shared__ __attribute__((aligned(16))) char lds[2][RS * D * 2 * QP];
+  __shared__ __attribute__((aligned(16))) float row_of[2][RS];
+  __shared__ __attribute__((aligned(16))) int seen_of[2][RS];
+  const CacheArgs& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int id = blockIdx.x;
+  const int h = id % c.H;
+  id /= c.H;
+  const int b = id % c.B;
+  id /= c.B;
+  const int sp = id % splits, first = id / splits * TOKENS;
+  const Seq s = sequence(c, b);
+  if (first >= s.len) return;
+  const int rows = rows_of(a, s, b), old = s.len - s.n, G = a.G;
+  const int64_t tb = c.q_start ? 0 : b;
+
+  // the work group's stages: those whose rows see its first token, an equal part of them
+  int begin = a.causal && first > old ? (first - old) * G / RS : 0;
+  const int all = (rows + RS - 1) / RS;
+  const int each = all > begin ? (all - begin + splits - 1) / splits : 0;
+  begin += sp * each;
+  const int end = begin + each < all ? begin + each : all;
+
+  // keys: half the lanes hold elements 0 .. 15 of a block, the others 16 .. 31
+  const int tok0 = first + 64 * wave;
+  bf16x8 kk[2][DB][2];
+  bool there[2];
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    const int t = (tok0 >> 5) + v;
+    const int64_t page = 32 * t < s.len ? page_of(c, b, t) : -1;
+    there[v] = page >= 0;
+    const char* p = c.data + tile_at(c, page < 0 ? 0 : page, h, t);
+    const int key = lane & 31;
+#pragma unroll
+    for (int w = 0; w < DB; ++w) {
+      u32x2 x = {0u, 0u};
+      uint32_t e = 0;
+      if (there[v]) {
+        x = *(const u32x2*)(p + w * 512 + key * 16 + 8 * half);
+        e = *(const uint8_t*)(p + k_exp_at(D, key, w));
+      }
+      kk[v][w][0] = decode8(x[0], scale_of(e, 0));
+      kk[v][w][1] = decode8(x[1], scale_of(e, 0));
+    }
+  }
+
+  // Rows on their way: unit u is chunk u / 16 % 4 of a block of row u % 16 of 16,
+  // so that neighbouring lanes write neighbouring 16 bytes of LDS.
+  constexpr int NV = sizeof(T) == 4 ? 2 : 1;
+  u32x4 in[NU][NV];
+  int tok_of[NU], g_of[NU];
+  const int r00 = begin * RS;
+#pragma unroll
+  for (int i = 0; i < NU; ++i) {
+    const int u = tid + i * NT, r = r00 + u / 64 / DB * 16 + (u & 15);
+    tok_of[i] = r / G, g_of[i] = r % G;
+  }
+  int my_tok = (r00 + tid) / G, my_g = (r00 + tid) % G;  // of the row whose LSE the thread brings
+  RowShift my = kBlindRow;
+  const int rs_q = RS / G, rs_r = RS % G;
+  auto advance = [&](int& tok, int& g) {
+    tok += rs_q, g += rs_r;
+    if (g >= G) g -= G, ++tok;
+  };
+  auto load = [&](int stage) {
+    const int r0 = stage * RS;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int u = tid + i * NT;
+      const int v = u >> 6, blk = v % DB, r = r0 + v / DB * 16 + (u & 15), e = 32 * blk + 8 * ((u >> 4) & 3);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) in[i][k] = u32x4{0u, 0u, 0u, 0u};
+      if ((UNITS % NT == 0 || u < UNITS) && r < rows) {
+        const T* p = (const T*)a.q.p + tb * a.q.b + int64_t(s.row0 + tok_of[i]) * a.q.l +
+                     int64_t(h * G + g_of[i]) * a.q.h + e;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) in[i][k] = ((const u32x4*)p)[k];
+      }
+      advance(tok_of[i], g_of[i]);
+    }
+    if (tid < RS) {
+      my = r0 + tid < rows ? row_shift(a, s, tb, h, my_tok, my_g) : kBlindRow;
+      advance(my_tok, my_g);
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+      const int u = tid + i * NT;
+      if (UNITS % NT != 0 && u >= UNITS) continue;
+      const int v = u >> 6, blk = v % DB, r = v / DB * 16 + (u & 15), ch = (u >> 4) & 3;
+      bf16x8 q[QP];
+      if constexpr (QP == 1) {
+        q[0] = __builtin_bit_cast(bf16x8, in[i][0]);
+      } else {
+        float x[8];
+        load_row8<T>((const T*)&in[i][0], x);
+        split8<QP>(x, q);
+      }
+      char* p = lds[buf] + (((r >> 5) * DB + blk) * 2 + (ch & 1)) * QP * 1024 + ((ch >> 1) * 32 + (r & 31)) * 16;
+#pragma unroll
+      for (int k = 0; k < QP; ++k) *(bf16x8*)(p + 1024 * k) = q[k];
+    }
+    if (tid < RS) row_of[buf][tid] = my.shift, seen_of[buf][tid] = my.seen;
+  };
+
+  float sum[2] = {0.f, 0.f};
+  auto compute = [&](int buf) {
+#pragma unroll
+    for (int rt = 0; rt < RS / 32; ++rt) {
+      const int see = seen_of[buf][32 * rt + (lane & 31)];
+      if (!__builtin_amdgcn_ballot_w64(see > tok0)) continue;
+      f32x16 x[2];
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[v][r] = 0.f;
+#pragma unroll
+      for (int w = 0; w < DB; ++w)
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int k = QP - 1; k >= 0; --k) {
+            const bf16x8 q = *(const bf16x8*)(lds[buf] + (((rt * DB + w) * 2 + st) * QP + k) * 1024 + lane * 16);
+#pragma unroll
+            for (int v = 0; v < 2; ++v) x[v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q, kk[v][w][st], x[v], 0, 0, 0);
+          }
+      const bool whole = !__builtin_amdgcn_ballot_w64(see < tok0 + 64);
+      float part[2][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 sh = *(const f32x4*)&row_of[buf][32 * rt + 8 * i + 4 * half];
+        float y[2][4];
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[v][e] = fast_exp2(__builtin_fmaf(x[v][4 * i + e], a.scale_log2, -sh[e]));
+        if (!whole) {
+          typedef __attribute__((__vector_size__(16))) int i32x4;
+          const i32x4 sn = *(const i32x4*)&seen_of[buf][32 * rt + 8 * i + 4 * half];
+#pragma unroll
+          for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (tok0 + 32 * v + (lane & 31) >= sn[e]) y[v][e] = 0.f;
+        }
+#pragma unroll
+        for (int v = 0; v < 2; ++v) part[v][i] = (y[v][0] + y[v][1]) + (y[v][2] + y[v][3]);
+      }
+#pragma unroll
+      for (int v = 0; v < 2; ++v) sum[v] += (part[v][0] + part[v][1]) + (part[v][2] + part[v][3]);
+    }
+  };
+
+  if (begin < end) {
+    load(begin);
+    put(0);
+    if (begin + 1 < end) load(begin + 1);
+  }
+  for (int stage = begin; stage < end; ++stage) {
+    const int buf = (stage - begin) & 1;
+    __syncthreads();
+    if (tok0 < s.len) compute(buf);
+    if (stage + 1 < end) {
+      put(buf ^ 1);
+      if (stage + 2 < end) load(stage + 2);
+    }
+  }
+
+  // the halves' lanes exchange: the lower half gets the first 32 tokens' sums
+  if (!there[0]) sum[0] = 0.f;
+  if (!there[1]) sum[1] = 0.f;
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, sum[0]),
+                                                  __builtin_bit_cast(uint32_t, sum[1]), false, false);
+  const uint32_t lo = r[0], hi = r[1];
+  const float y = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+  const int tok = tok0 + lane;
+  if (tok >= s.len) return;
+  if (splits > 1) {
+    a.part[(int64_t(sp) * c.B + b) * c.H * c.max_len + int64_t(h) * c.max_len + tok] = y;
+    return;
+  }
+  const float had = a.prior.p && tok < old ? a.prior.p[b * a.prior.b + h * a.prior.h + tok] : 0.f;
+  a.w.p[b * a.w.b + h * a.w.h + tok] = __builtin_fmaf(a.decay, had, y);
+}
+
+// Adds the parts of a split call, in their order.
+__global__ void __launch_bounds__(256) cache_weigh_join(const WeighArgs a, int pieces, int splits) {
+  const CacheArgs& c = a.c;
+  const int64_t bh = blockIdx.x / pieces;
+  const int b = int(bh / c.H), h = int(bh % c.H);
+  const Seq s = sequence(c, b);
+  for (int tok = blockIdx.x % pieces * 256 + threadIdx.x; tok < s.len; tok += 256 * pieces) {
+    float y = 0.f;
+    for (int i = 0; i < splits; ++i) y += a.part[(int64_t(i) * c.B * c.H + bh) * c.max_len + tok];
+    const float had = a.prior.p && tok < s.len - s.n ? a.prior.p[b * a.prior.b + h * a.prior.h + tok] : 0.f;
+    a.w.p[b * a.w.b + h * a.w.h + tok] = __builtin_fmaf(a.decay, had, y);
   }
 }
 
 namespace {
 
+// Rows of a stage, so that two of them fit LDS.
+constexpr int stage_rows(int parts, int db) { return parts * db <= 8 ? 64 : 32; }
+constexpr int kManyWaves = 8;
+
+template <typename T, int DB>
+void launch_d(const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
+  constexpr int QP = RowType<T>::kQuery, NQ = weigh_few_groups(QP, DB);
+  const dim3 grid(unsigned(p.groups));
+  if (p.many) {
+    hipLaunchKernelGGL((cache_weigh_many<T, DB, kManyWaves, stage_rows(QP, DB)>), grid, dim3(64 * kManyWaves), 0, s, a,
+                       p.tiles, p.splits);
+  } else if (p.row_groups == 1) {
+    hipLaunchKernelGGL((cache_weigh_few<T, DB, 1>), grid, dim3(256), 0, s, a, p.tiles);
+  } else if constexpr (NQ == 2) {
+    hipLaunchKernelGGL((cache_weigh_few<T, DB, 2>), grid, dim3(256), 0, s, a, p.tiles);
+  }
+}
+
 template <typename T>
-hipError_t launch_rows(const WeighArgs& a, hipStream_t s) {
-  const int64_t heads = int64_t(a.c.B) * a.c.H;
-  int64_t per = (int64_t(a.c.max_len) + 127) / 128;
-  const int64_t most = (int64_t(1) << 23) / heads;  // heads are at most 2^23
-  if (per > most) per = most;
-  const dim3 grid(unsigned(per * heads));
+hipError_t launch_rows(const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
   switch (a.c.d / 32) {
-#define CQSA_WEIGH(DB)                                                                              \
-  case DB:                                                                                          \
-    hipLaunchKernelGGL((cache_weigh_rows<T, DB>), grid, dim3(256), 0, s, a, int(per));              \
+#define CQSA_WEIGH(DB)        \
+  case DB:                    \
+    launch_d<T, DB>(a, p, s); \
     break;
     CQSA_WEIGH(1)
     CQSA_WEIGH(2)
@@ -116,15 +436,49 @@ hipError_t launch_rows(const WeighArgs& a, hipStream_t s) {
     CQSA_WEIGH(8)
 #undef CQSA_WEIGH
   }
+  if (p.splits > 1) {
+    const int64_t heads = int64_t(a.c.B) * a.c.H;
+    const int64_t pieces = std::min<int64_t>((int64_t(a.c.max_len) + 255) / 256, (int64_t(1) << 23) / heads);
+    hipLaunchKernelGGL(cache_weigh_join, dim3(unsigned(pieces * heads)), dim3(256), 0, s, a, int(pieces), p.splits);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cache_weigh(cqsa_dtype dt, const WeighArgs& a, hipStream_t s) {
-  if (dt == CQSA_BF16) return launch_rows<__bf16>(a, s);
-  if (dt == CQSA_F16) return launch_rows<_Float16>(a, s);
-  return launch_rows<float>(a, s);
+WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d) {
+  WeighPlan p{};
+  const int parts = dt == CQSA_F32 ? 3 : (dt == CQSA_F16 ? 2 : 1), db = d / 32;
+  const int64_t heads = B * H;
+  p.splits = 1;
+  p.many = rows > 16 * weigh_few_groups(parts, db);
+  if (p.many) {
+    const int64_t stages = (rows + stage_rows(parts, db) - 1) / stage_rows(parts, db);
+    p.tiles = int((max_len + 64 * kManyWaves - 1) / (64 * kManyWaves));
+    const int64_t groups = heads * p.tiles;
+    p.splits = int(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(stages / 2, 64), 512 / groups)));
+    p.groups = groups * p.splits;
+    return p;
+  }
+  p.row_groups = rows > 16 ? 2 : 1;
+  // Work groups a sequence and head: as many as the GPU holds at once, or of several
+  // sequences, whose lengths differ, one for every 8 tiles of its waves with one group
+  // of rows and 16 with two, so that the long ones' parts even out (64 of up to
+  // 16384 tokens, 8 heads, d = 128: 67 us, with as many as fit 81; 16 of them 20 and 20;
+  // one of 2^20 126, in parts of 8 tiles 138; 64 of up to 16384, two groups of rows, 98 and 101).
+  const int64_t tiles = (max_len + 31) / 32, most = (tiles + 3) / 4;
+  const int held = parts * db * p.row_groups;
+  const int64_t fit = (held <= 4 ? 1536 : held <= 12 ? 1024 : 768) / heads;
+  const int64_t even = B == 1 ? 0 : tiles / (32 * p.row_groups);
+  p.tiles = int(std::max<int64_t>(1, std::min(most, std::max(fit, even))));
+  p.groups = heads * p.tiles;
+  return p;
+}
+
+hipError_t launch_cache_weigh(cqsa_dtype dt, const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
+  if (dt == CQSA_BF16) return launch_rows<__bf16>(a, p, s);
+  if (dt == CQSA_F16) return launch_rows<_Float16>(a, p, s);
+  return launch_rows<float>(a, p, s);
 }
 
 }  // namespace cqsa
