@@ -36,6 +36,12 @@ struct WeighPlan {
 // rows: the most that a sequence and key head has.
 WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
 
+// The key at which a head's kept tokens end.
+struct EvictBorder {
+  uint32_t key;  // its digits so far
+  int left;      // keys to take among those that share them
+};
+
 struct EvictArgs {
   CacheArgs c;  // the cache and the sequences as they are
   TokenWeights w, w_to;
@@ -49,11 +55,21 @@ struct EvictArgs {
   bool pad;             // -1 behind the kept tokens' positions
   int32_t* n_kept;      // [B], workspace
   int32_t* new_lengths;
+  // heads that work groups share, chunk by chunk
+  int chunks;           // 0: they do not
+  uint32_t* counts;     // EvictPlan::counts words
+  EvictBorder* state;   // [B, H, 3]
+  int2* chunk_counts;   // [B, H, chunks]: keys above the border, and equal to it
   char* stage;          // in place: [B, H, ceil(cap / 32)] tiles,
   float* stage_w;       // and [B, H, cap] weights
 };
 
 hipError_t launch_cache_weigh(cqsa_dtype dt, const WeighArgs& a, const WeighPlan& p, hipStream_t s);
+struct EvictPlan {
+  int chunks;
+  int64_t counts;
+};
+EvictPlan plan_evict(int64_t B, int64_t H, int64_t max_len);
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t s);
 
 }  // namespace cqsa

@@ -310,7 +310,8 @@ cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqs
 // Parts of an eviction's workspace, each 16-byte aligned, by the sizes of its arguments.
 struct EvictSpace {
   int64_t cap, tiles;
-  uint64_t n_kept, kept, stage, stage_w, bytes;
+  EvictPlan plan;
+  uint64_t n_kept, kept, counts, state, chunk_counts, stage, stage_w, bytes;
 };
 EvictSpace evict_space(const cqsa_cache* c, const cqsa_cache_batch* b, int32_t budget, bool in_place) {
   EvictSpace e{};
@@ -324,6 +325,10 @@ EvictSpace evict_space(const cqsa_cache* c, const cqsa_cache_batch* b, int32_t b
   };
   e.n_kept = part(4 * uint64_t(b->B));
   e.kept = part(4 * heads * uint64_t(e.cap));
+  e.plan = plan_evict(b->B, c->H, b->max_len);
+  e.counts = part(4 * uint64_t(e.plan.counts));
+  e.state = part(e.plan.chunks ? heads * 3 * sizeof(EvictBorder) : 0);
+  e.chunk_counts = part(heads * uint64_t(e.plan.chunks) * sizeof(int2));
   e.stage = part(in_place ? heads * uint64_t(e.tiles) * uint64_t(tile_bytes(c->d)) : 0);
   e.stage_w = part(in_place ? 4 * heads * uint64_t(e.cap) : 0);
   return e;
@@ -397,6 +402,10 @@ cqsa_status evict_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqs
   a.pad = kept != nullptr;
   a.n_kept = (int32_t*)(space + e.n_kept);
   a.new_lengths = new_lengths;
+  a.chunks = e.plan.chunks;
+  a.counts = (uint32_t*)(space + e.counts);
+  a.state = (EvictBorder*)(space + e.state);
+  a.chunk_counts = (int2*)(space + e.chunk_counts);
   a.stage = space + e.stage;
   a.stage_w = (float*)(space + e.stage_w);
   CQSA_HIP(launch_cache_evict(a, s));

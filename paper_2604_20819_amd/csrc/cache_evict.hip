@@ -3,8 +3,12 @@
 //
 // A token's rank is a 32-bit key: 0 where its page holds nothing, 1 for a NaN, the
 // weight's bits in an order that integers compare by, and 2^32 - 1 for the first and
-// the recent tokens.  The n-th largest key is found by its digits, from counts of
-// the keys that share its upper ones.
+// the recent tokens.  The n-th largest key is found by its digits of 11, 11 and 10
+// bits, from counts of the keys that share its upper ones: integers, whose sums go in
+// any order.  A head's tokens up to 16384 are a work group's, which holds their keys in
+// registers; longer ones are shared by many, with the counts in memory.
+#include <algorithm>
+
 #include "cache_bound.hpp"
 #include "hip_common.hpp"
 
@@ -13,6 +17,11 @@ namespace cqsa {
 namespace {
 
 constexpr uint32_t kForced = 0xffffffffu;
+constexpr int kItems = 16;    // keys of a lane
+constexpr int kBins = 2048;   // of a digit
+constexpr int kChunk = 4096;  // tokens of a work group that shares a head with others
+// words of a head in memory: three digits' counts, and how many tokens have no page
+constexpr int kHeadWords = 3 * kBins + 4;
 
 __device__ __forceinline__ uint32_t rank_of(float w) {
   uint32_t u = __builtin_bit_cast(uint32_t, w);
@@ -27,148 +36,393 @@ __device__ __forceinline__ int length_of(const CacheArgs& c, int b) {
   return n < 0 ? 0 : (n > c.max_len ? c.max_len : n);
 }
 
-__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, const float* w, int b, int len, int t) {
-  if (t >= len || page_of(a.c, b, t >> 5) < 0) return 0u;
-  return t < a.first || t >= len - a.recent ? kForced : rank_of(w[t]);
+// Keys of the wave's tokens t0 + 64 i + lane; behind the sequence 0.
+__device__ __forceinline__ void load_keys(const EvictArgs& a, const float* w, int b, int len, int t0, int lane,
+                                          uint32_t* key) {
+  float x[kItems];
+  int32_t page[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int t = t0 + 64 * i + lane;
+    x[i] = t < len ? w[t] : 0.f;
+    page[i] = t < len ? a.c.pages[b * a.c.pages_stride + (t >> a.c.page_log2)] : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const int t = t0 + 64 * i + lane;
+    const bool forced = t < a.first || t >= len - a.recent;
+    key[i] = page[i] < 0 || page[i] >= a.c.n_pages ? 0u : forced ? kForced : rank_of(x[i]);
+  }
 }
+
+// A digit of a key, from the uppermost on: 11, 11 and 10 bits.
+__device__ __forceinline__ uint32_t digit_of(uint32_t k, int pass) {
+  return pass == 0 ? k >> 21 : pass == 1 ? k >> 10 & 2047u : k & 1023u;
+}
+// Whether k has the border's upper digits.
+__device__ __forceinline__ bool shares(uint32_t k, uint32_t border, int pass) {
+  return pass == 0 || (pass == 1 ? k >> 21 == border >> 21 : k >> 10 == border >> 10);
+}
+
+// The digit in which the `left`-th largest of the counted keys lies: counts of kBins in
+// `count` (LDS or memory), by the NT threads of a work group.  `scratch`: a word a wave and 2.
+template <int NT>
+__device__ __forceinline__ EvictBorder next_digit(const uint32_t* count, const EvictBorder& at, int pass, int* scratch) {
+  constexpr int PER = kBins / NT, WAVES = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int mine[PER], sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sum += mine[i] = int(count[kBins - 1 - (tid * PER + i)]);  // from the largest down
+  int run = sum;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const int y = __shfl_up(run, k);
+    if (lane >= k) run += y;
+  }
+  if (lane == 63) scratch[wave] = run;
+  __syncthreads();
+  int above = run - sum;
+  for (int i = 0; i < WAVES; ++i) above += i < wave ? scratch[i] : 0;
+  if (above < at.left && above + sum >= at.left) {  // one thread's, if left is 1 or more
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (above < at.left && above + mine[i] >= at.left) {
+        scratch[WAVES] = kBins - 1 - (tid * PER + i);
+        scratch[WAVES + 1] = at.left - above;
+      }
+      above += mine[i];
+    }
+  }
+  __syncthreads();
+  const uint32_t d = uint32_t(scratch[WAVES]);
+  const EvictBorder next = {at.key | (pass == 0 ? d << 21 : pass == 1 ? d << 10 : d), scratch[WAVES + 1]};
+  __syncthreads();
+  return next;
+}
+
+// Places of a wave's kept keys: above the border, or among the first `left` that equal it,
+// with n0 and n1 such keys before the wave's.
+__device__ __forceinline__ void place(const uint32_t* key, const EvictBorder& at, int t0, int lane, int n0, int n1,
+                                      int32_t* kept) {
+  const uint64_t below = (uint64_t(1) << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    const uint64_t above = __builtin_amdgcn_ballot_w64(key[i] > at.key);
+    const uint64_t equal = __builtin_amdgcn_ballot_w64(key[i] == at.key);
+    const int m0 = n0 + __builtin_popcountll(above & below), m1 = n1 + __builtin_popcountll(equal & below);
+    if (key[i] > at.key)
+      kept[m0 + (m1 < at.left ? m1 : at.left)] = t0 + 64 * i + lane;
+    else if (key[i] == at.key && m1 < at.left)
+      kept[m0 + m1] = t0 + 64 * i + lane;
+    n0 += __builtin_popcountll(above), n1 += __builtin_popcountll(equal);
+  }
+}
+
+__device__ __forceinline__ void count_keys(const uint32_t* key, const EvictBorder& at, int* n0, int* n1) {
+  *n0 = *n1 = 0;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    *n0 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] > at.key));
+    *n1 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] == at.key));
+  }
+}
+
+constexpr EvictBorder kNothing = {kForced, 0};  // of a sequence that keeps nothing
+
+__device__ __forceinline__ int kept_of(const EvictArgs& a, int present) { return present < a.budget ? present : a.budget; }
 
 }  // namespace
 
-// One work group a sequence and head.
-__global__ void __launch_bounds__(1024) cache_evict_select(const EvictArgs a) {
-  __shared__ uint32_t count[256];
-  __shared__ uint32_t found[2];
-  __shared__ int per_wave[2][16];
-  const int id = (blockIdx.y << kGridLog2) + blockIdx.x;
-  const int h = id % a.c.H, b = id / a.c.H;
+// A work group of WAVES takes all of a head's tokens, 1024 a wave.
+template <int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) cache_evict_select(const EvictArgs a) {
+  constexpr int NT = 64 * WAVES;
+  __shared__ uint32_t count[kBins];
+  __shared__ int scratch[WAVES + 2];
+  __shared__ int before[2][WAVES];
+  const int64_t id = (int64_t(blockIdx.y) << kGridLog2) + blockIdx.x;
+  const int h = int(id % a.c.H), b = int(id / a.c.H);
   if (b >= a.c.B) return;  // the grid has two dimensions
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = length_of(a.c, b);
   const float* w = a.w.p + b * a.w.b + h * a.w.h;
-  uint32_t prefix = 0, left = 0;  // the border's upper digits; keys still to find at it
-  int keep = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) count[tid] = 0;
+  const int t0 = 1024 * wave;
+  uint32_t key[kItems];
+  load_keys(a, w, b, len, t0, lane, key);
+  int present = 0;
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) present += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] != 0u));
+  if (lane == 0) before[0][wave] = present;
+  EvictBorder at = {0u, 0};
+  for (int pass = 0; pass < 3; ++pass) {
+    for (int i = tid; i < kBins; i += NT) count[i] = 0;
     __syncthreads();
-    uint32_t absent = 0;
-    for (int t = tid; t < len; t += 1024) {
-      const uint32_t k = key_of(a, w, b, len, t);
-      absent += k == 0u;
-      if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&count[k >> shift & 255u], 1u);
+    if (pass == 0) {
+      present = 0;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) present += before[0][i];
+      at.left = kept_of(a, present);
+      if (at.left == 0) break;
     }
-    if (shift == 24) {
-      if (tid == 0) found[0] = 0;
-      __syncthreads();
-      if (absent) atomicAdd(&found[0], absent);
-      __syncthreads();
-      const int present = len - int(found[0]);
-      keep = present < a.budget ? present : a.budget;
-      left = uint32_t(keep);
-    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+      if (key[i] != 0u && shares(key[i], at.key, pass)) atomicAdd(&count[digit_of(key[i], pass)], 1u);
     __syncthreads();
-    if (tid == 0) {
-      uint32_t above = 0;
-      int d = 255;
-      while (d > 0 && above + count[d] < left) above += count[d--];
-      found[0] = uint32_t(d), found[1] = above;
-    }
-    __syncthreads();
-    prefix = prefix << 8 | found[0];
-    left -= found[1];
-    __syncthreads();
+    at = next_digit<NT>(count, at, pass, scratch);
   }
-  if (keep == 0) prefix = kForced, left = 0;
-  // keys above the border are kept, and the first `left` that equal it
-  int32_t* kept = a.kept + (int64_t(b) * a.c.H + h) * a.kept_stride;
-  int done = 0, ties = 0;
-  for (int t0 = 0; t0 < len; t0 += 1024) {
-    const int t = t0 + tid;
-    const uint32_t k = key_of(a, w, b, len, t);
-    const uint64_t above = __builtin_amdgcn_ballot_w64(k > prefix), equal = __builtin_amdgcn_ballot_w64(k == prefix && k != 0u);
-    if (lane == 0) per_wave[0][wave] = __builtin_popcountll(above), per_wave[1][wave] = __builtin_popcountll(equal);
-    __syncthreads();
-    int n0 = done, n1 = ties, all0 = 0, all1 = 0;
-    for (int i = 0; i < 16; ++i) {
-      if (i < wave) n0 += per_wave[0][i], n1 += per_wave[1][i];
-      all0 += per_wave[0][i], all1 += per_wave[1][i];
-    }
-    const uint64_t below = (uint64_t(1) << lane) - 1;
-    n0 += __builtin_popcountll(above & below), n1 += __builtin_popcountll(equal & below);
-    const int lim = int(left);
-    const bool mine = k > prefix || (k == prefix && k != 0u && n1 < lim);
-    if (mine) kept[n0 + (n1 < lim ? n1 : lim)] = t;
-    done += all0, ties += all1;
-    __syncthreads();
-  }
+  const int keep = kept_of(a, present);
+  if (keep == 0) at = kNothing;
+  int n0, n1;
+  count_keys(key, at, &n0, &n1);
+  __syncthreads();
+  if (lane == 0) before[0][wave] = n0, before[1][wave] = n1;
+  __syncthreads();
+  n0 = n1 = 0;
+  for (int i = 0; i < wave; ++i) n0 += before[0][i], n1 += before[1][i];
+  int32_t* kept = a.kept + id * a.kept_stride;
+  place(key, at, t0, lane, n0, n1, kept);
   if (a.pad)
-    for (int i = keep + tid; i < a.budget; i += 1024) kept[i] = -1;
+    for (int i = keep + tid; i < a.budget; i += NT) kept[i] = -1;
   if (h == 0 && tid == 0) a.n_kept[b] = keep;
 }
 
-// A work group for each 32 kept tokens.  STAGED: from the stage into the pages, in
-// their places; else from the pages into the stage (in place) or the target's pages.
+// ------------------------------------------------- heads that work groups share
+// A head has `per` work groups, one for each chunk of kChunk tokens, or fewer where there
+// are very many.
+__global__ void __launch_bounds__(256) cache_evict_clear(uint32_t* words, int64_t n) {
+  for (int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4; i < n; i += int64_t(gridDim.x) * 1024)
+    *(u32x4*)(words + i) = u32x4{0u, 0u, 0u, 0u};
+}
+
+// The border so far: by the counts of the pass before, with the digits that its own work groups
+// left in `state`.  The first chunk's work group leaves it there in turn.
+template <int PASS>
+__device__ __forceinline__ EvictBorder border_of(const EvictArgs& a, int64_t id, int len, bool leave, int* scratch) {
+  uint32_t* words = a.counts + id * kHeadWords;
+  if (PASS == 0) return {0u, 0};
+  EvictBorder at;
+  if (PASS == 1) {
+    at = {0u, kept_of(a, len - int(words[3 * kBins]))};
+  } else {
+    at = a.state[id * 3 + PASS - 2];
+  }
+  if (at.left == 0) {
+    at = kNothing;
+  } else {
+    at = next_digit<256>(words + (PASS - 1) * kBins, at, PASS - 1, scratch);
+  }
+  if (leave && threadIdx.x == 0) a.state[id * 3 + PASS - 1] = at;
+  return at;
+}
+
+template <int PASS>
+__global__ void __launch_bounds__(256) cache_evict_count(const EvictArgs a, int per) {
+  __shared__ uint32_t count[kBins];
+  __shared__ int scratch[6];
+  const int64_t id = blockIdx.x / per;
+  const int part = blockIdx.x % per;
+  const int h = int(id % a.c.H), b = int(id / a.c.H);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int len = length_of(a.c, b);
+  const EvictBorder at = border_of<PASS>(a, id, len, part == 0, scratch);
+  const float* w = a.w.p + b * a.w.b + h * a.w.h;
+  uint32_t* words = a.counts + id * kHeadWords;
+  if (PASS < 3) {
+    for (int i = tid; i < kBins; i += 256) count[i] = 0;
+    __syncthreads();
+  }
+  int absent = 0;
+  for (int chunk = part; chunk < a.chunks; chunk += per) {
+    const int t0 = chunk * kChunk + 1024 * wave;
+    uint32_t key[kItems];
+    int n0 = 0, n1 = 0;
+    if (t0 < len) {
+      load_keys(a, w, b, len, t0, lane, key);
+      if (PASS == 3) {
+        count_keys(key, at, &n0, &n1);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+          if (PASS == 0) absent += key[i] == 0u && t0 + 64 * i + lane < len;
+          if (key[i] != 0u && shares(key[i], at.key, PASS)) atomicAdd(&count[digit_of(key[i], PASS)], 1u);
+        }
+      }
+    }
+    if (PASS == 3) {
+      __syncthreads();
+      if (lane == 0) scratch[wave] = n0, count[wave] = uint32_t(n1);
+      __syncthreads();
+      if (tid == 0) {
+        a.chunk_counts[id * a.chunks + chunk] =
+            int2{scratch[0] + scratch[1] + scratch[2] + scratch[3], int(count[0] + count[1] + count[2] + count[3])};
+      }
+    }
+  }
+  if (PASS == 3) return;
+  if (PASS == 0 && absent) atomicAdd(&words[3 * kBins], uint32_t(absent));
+  __syncthreads();
+  for (int i = tid; i < kBins; i += 256)
+    if (count[i]) atomicAdd(&words[PASS * kBins + i], count[i]);
+}
+
+__global__ void __launch_bounds__(256) cache_evict_place(const EvictArgs a, int per) {
+  __shared__ int before[2][4], own[2][4];
+  const int64_t id = blockIdx.x / per;
+  const int part = blockIdx.x % per;
+  const int h = int(id % a.c.H), b = int(id / a.c.H);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int len = length_of(a.c, b);
+  const EvictBorder at = a.state[id * 3 + 2];
+  const int keep = kept_of(a, len - int(a.counts[id * kHeadWords + 3 * kBins]));
+  const float* w = a.w.p + b * a.w.b + h * a.w.h;
+  int32_t* kept = a.kept + id * a.kept_stride;
+  const int2* chunks = a.chunk_counts + id * a.chunks;
+  int from = 0, sum0 = 0, sum1 = 0;  // keys of the chunks before, this thread's part of them
+  for (int chunk = part; int64_t(chunk) * kChunk < len; chunk += per) {
+    const int t0 = chunk * kChunk + 1024 * wave;
+    uint32_t key[kItems];
+    load_keys(a, w, b, len, t0, lane, key);
+    for (int i = from + tid; i < chunk; i += 256) {
+      const int2 x = chunks[i];
+      sum0 += x.x, sum1 += x.y;
+    }
+    from = chunk;
+    int m0 = sum0, m1 = sum1;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) m0 += __shfl_xor(m0, k), m1 += __shfl_xor(m1, k);
+    int n0, n1;
+    count_keys(key, at, &n0, &n1);
+    __syncthreads();
+    if (lane == 0) before[0][wave] = m0, before[1][wave] = m1, own[0][wave] = n0, own[1][wave] = n1;
+    __syncthreads();
+    n0 = n1 = 0;
+    for (int i = 0; i < 4; ++i) {
+      n0 += before[0][i], n1 += before[1][i];
+      if (i < wave) n0 += own[0][i], n1 += own[1][i];
+    }
+    place(key, at, t0, lane, n0, n1, kept);
+  }
+  if (a.pad)
+    for (int64_t i = keep + int64_t(part) * 256 + tid; i < a.budget; i += int64_t(per) * 256) kept[i] = -1;
+  if (h == 0 && part == 0 && tid == 0) a.n_kept[b] = keep;
+}
+
+// --------------------------------------------------------------------- moving
+// A wave moves 32 kept tokens of a head.  STAGED: from the stage into the pages, in their
+// places; else from the pages into the stage (in place) or the target's pages.  A lane's four
+// source tokens are the same for all channel pairs, whose 4 bytes it gathers one by one:
+// the cache holds values by channel pairs, so that any token moved touches all of its tile.
 template <bool STAGED>
 __global__ void __launch_bounds__(256) cache_evict_move(const EvictArgs a, int tiles) {
-  __shared__ const char* from[32];
-  __shared__ int at[32];
   const CacheArgs& c = a.c;
-  const int d = c.d, db = d >> 5, tid = threadIdx.x;
-  const int id = (blockIdx.y << kGridLog2) + blockIdx.x;
-  const int tile = id % tiles;
+  const int d = c.d, db = d >> 5, lane = threadIdx.x & 63, low = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = ((int64_t(blockIdx.y) << kGridLog2) + blockIdx.x) * 4 + wave;
+  const int tile = int(id % tiles);
   const int64_t bh = id / tiles;
   const int h = int(bh % c.H), b = int(bh / c.H);
-  if (b >= c.B) return;  // the grid has two dimensions
+  if (b >= c.B) return;  // behind the last tile
   const int keep = a.n_kept[b];
-  if (h == 0 && tile == 0 && tid == 0 && (STAGED || !a.in_place)) a.new_lengths[b] = keep;
+  if (h == 0 && tile == 0 && lane == 0 && (STAGED || !a.in_place)) a.new_lengths[b] = keep;
   const int n = keep - 32 * tile < 32 ? keep - 32 * tile : 32;
   if (n <= 0) return;
-  const int32_t* kept = a.kept + bh * a.kept_stride + 32 * tile;
+  const int t = low < n ? a.kept[bh * a.kept_stride + 32 * tile + low] : -1;
+  // in place: tokens that stay where they are
+  if (a.in_place && !__builtin_amdgcn_ballot_w64(low < n && t != 32 * tile + low)) return;
   char* const stage = a.stage + (bh * tiles + tile) * tile_bytes(d);
-  // where the tile goes
+  if (lane < n) {
+    const float* w = a.w.p + b * a.w.b + h * a.w.h;
+    const int64_t i = bh * a.cap + 32 * tile + lane;
+    if (STAGED)
+      a.w.p[b * a.w.b + h * a.w.h + 32 * tile + lane] = a.stage_w[i];
+    else if (a.in_place)
+      a.stage_w[i] = w[t];
+    else if (a.w_to.p)
+      a.w_to.p[b * a.w_to.b + h * a.w_to.h + 32 * tile + lane] = w[t];
+  }
   char* dst = stage;
   if (STAGED || !a.in_place) {
     const int32_t* table = STAGED ? c.pages + b * c.pages_stride : a.to_pages + b * a.to_stride;
     const int32_t p = table[tile >> (c.page_log2 - 5)];
-    dst = p >= 0 && p < c.n_pages ? c.data + tile_at(c, p, h, tile) : nullptr;
+    if (p < 0 || p >= c.n_pages) return;  // no such page: dropped
+    dst = c.data + tile_at(c, p, h, tile);
   }
-  if (tid < 32) {
-    const int t = tid < n ? kept[tid] : 0;
-    from[tid] = STAGED ? stage : tid < n ? c.data + tile_at(c, page_of(c, b, t >> 5), h, t >> 5) : nullptr;
-    at[tid] = STAGED ? tid : t & 31;
-    if (tid < n) {
-      const int64_t i = bh * a.cap + 32 * tile + tid;
-      if (STAGED)
-        a.w.p[b * a.w.b + h * a.w.h + 32 * tile + tid] = a.stage_w[i];
-      else if (a.in_place)
-        a.stage_w[i] = a.w.p[b * a.w.b + h * a.w.h + t];
-      else if (a.w_to.p)
-        a.w_to.p[b * a.w_to.b + h * a.w_to.h + 32 * tile + tid] = a.w.p[b * a.w.b + h * a.w.h + t];
-    }
+  if (STAGED && n == 32) {
+    const int vecs = 34 * d / 16;
+    for (int i = lane; i < vecs; i += 64) ((u32x4*)dst)[i] = ((const u32x4*)stage)[i];
+    return;
   }
-  __syncthreads();
-  if (!dst) return;
-  for (int u = tid; u < 32 * db; u += 256) {  // keys' codes: a token's block
-    const int tok = u & 31, blk = u >> 5;
-    if (tok < n) *(u32x4*)(dst + k_code_at(d, tok, blk, 0)) = *(const u32x4*)(from[tok] + k_code_at(d, at[tok], blk, 0));
+  // this lane's token `low`, as keys have it, and the four of its word of values
+  const int src = low < n ? t : 0;
+  const int64_t from = STAGED || low >= n ? 0 : tile_at(c, page_of(c, b, src >> 5), h, src >> 5);
+  const char* const base = STAGED ? stage : c.data;
+  const int at = STAGED ? low : src & 31;
+  const int word = lane & 7, first = 16 * (word & 1) + 4 * (word >> 1);
+  const char* v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int tok = first + k < n ? first + k : 0;
+    const int64_t o = int64_t(uint32_t(__shfl(int(from), tok))) | int64_t(__shfl(int(from >> 32), tok)) << 32;
+    v[k] = base + o + 16 * d + v_token_at(__shfl(at, tok)) + 32 * (lane >> 3);
   }
-  for (int u = tid; u < 16 * d; u += 256) {  // values' codes: a token's channel pair
-    const int tok = u & 31, i = u >> 5;  // i: 16 blk + pair
-    if (tok < n) dst[v_code_at(d, tok, i >> 4, i & 15)] = from[tok][v_code_at(d, at[tok], i >> 4, i & 15)];
+  const char* const k0 = base + from;
+#pragma unroll 2
+  for (int blk = lane >> 5; blk < db; blk += 2) {
+    if (low >= n) continue;
+    *(u32x4*)(dst + k_code_at(d, low, blk, 0)) = *(const u32x4*)(k0 + k_code_at(d, at, blk, 0));
+    dst[k_exp_at(d, low, blk)] = k0[k_exp_at(d, at, blk)];
+    dst[v_exp_at(d, low, blk)] = k0[v_exp_at(d, at, blk)];
   }
-  for (int u = tid; u < d; u += 256) {
-    const int tok = u & 31, blk = u >> 5;
-    if (tok < n) {
-      dst[k_exp_at(d, tok, blk)] = from[tok][k_exp_at(d, at[tok], blk)];
-      dst[v_exp_at(d, tok, blk)] = from[tok][v_exp_at(d, at[tok], blk)];
+  char* const out = dst + 16 * d + 32 * (lane >> 3) + 4 * word;
+  const bool full = first + 3 < n;
+#pragma unroll 4
+  for (int i = 0; i < 2 * db; ++i) {  // 8 of the 16 db channel pairs
+    uint32_t x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = uint8_t(v[k][256 * i]);
+    if (full) {
+      *(uint32_t*)(out + 256 * i) = x[0] | x[1] << 8 | x[2] << 16 | x[3] << 24;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (first + k < n) out[256 * i + k] = char(x[k]);
     }
   }
 }
 
+// ------------------------------------------------------------------ launching
+EvictPlan plan_evict(int64_t B, int64_t H, int64_t max_len) {
+  EvictPlan p{};
+  if (max_len <= 16 * 1024) return p;
+  p.chunks = int((max_len + kChunk - 1) / kChunk);
+  p.counts = B * H * kHeadWords;
+  return p;
+}
+
 hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t s) {
   const int64_t heads = int64_t(a.c.B) * a.c.H;
-  hipLaunchKernelGGL(cache_evict_select, attend_grid(heads), dim3(1024), 0, s, a);
+  if (a.chunks == 0) {
+    if (a.c.max_len <= 4096)
+      hipLaunchKernelGGL((cache_evict_select<4>), attend_grid(heads), dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((cache_evict_select<16>), attend_grid(heads), dim3(1024), 0, s, a);
+  } else {
+    const int64_t words = heads * kHeadWords;
+    const int per = int(std::min<int64_t>(a.chunks, std::max<int64_t>(1, (int64_t(1) << 22) / heads)));
+    const dim3 grid(unsigned(heads * per));
+    hipLaunchKernelGGL(cache_evict_clear, dim3(unsigned(std::min<int64_t>((words + 1023) / 1024, 1 << 16))), dim3(256), 0, s,
+                       a.counts, words);
+    hipLaunchKernelGGL((cache_evict_count<0>), grid, dim3(256), 0, s, a, per);
+    hipLaunchKernelGGL((cache_evict_count<1>), grid, dim3(256), 0, s, a, per);
+    hipLaunchKernelGGL((cache_evict_count<2>), grid, dim3(256), 0, s, a, per);
+    hipLaunchKernelGGL((cache_evict_count<3>), grid, dim3(256), 0, s, a, per);
+    hipLaunchKernelGGL(cache_evict_place, grid, dim3(256), 0, s, a, per);
+  }
   const int tiles = a.cap > 0 ? (a.cap + 31) / 32 : 1;
-  const dim3 grid = attend_grid(heads * tiles);
+  const dim3 grid = attend_grid((heads * tiles + 3) / 4);
   hipLaunchKernelGGL((cache_evict_move<false>), grid, dim3(256), 0, s, a, tiles);
   if (a.in_place) hipLaunchKernelGGL((cache_evict_move<true>), grid, dim3(256), 0, s, a, tiles);
   return hipGetLastError();
