@@ -234,16 +234,6 @@ TokenWeights weights_of(const cqsa_weights* w) {
   return w ? TokenWeights{w->data, w->stride_b, w->stride_h} : TokenWeights{nullptr, 0, 0};
 }
 
-cqsa_status check_workspace(const void* p, uint64_t bytes, uint64_t need, const std::string& what) {
-  if (need == 0) return CQSA_OK;
-  if (!p || bytes < need)
-    return fail(CQSA_ERR_INVALID_ARG, what + "the workspace has " + std::to_string(p ? bytes : 0) +
-                                          " bytes, the call needs " + std::to_string(need));
-  if (reinterpret_cast<uintptr_t>(p) % 16 != 0)
-    return fail(CQSA_ERR_INVALID_ARG, what + "the workspace must be 16-byte aligned");
-  return CQSA_OK;
-}
-
 // The launch of a call whose arguments check_attend has passed, and its workspace.
 WeighPlan weigh_plan(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view& Q) {
   const int64_t n = empty(Q) ? 0 : b->q_start ? b->max_q : Q.L;

@@ -17,7 +17,10 @@ struct VerifyArgs {
   const int32_t* lengths;
   int32_t* new_lengths;
   int32_t B, K, V;
+  void* sums;  // workspace of verify_bytes
 };
+
+uint64_t verify_bytes(int64_t B, int64_t V, cqsa_dtype dt);
 
 hipError_t launch_verify(cqsa_dtype dt, const VerifyArgs& a, hipStream_t s);
 

@@ -32,6 +32,16 @@ inline Range range_of(const char* name, const void* p, uint64_t bytes) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
   return {name, at, p ? at + bytes : at};
 }
+inline cqsa_status check_workspace(const void* p, uint64_t bytes, uint64_t need, const std::string& what) {
+  if (need == 0) return CQSA_OK;
+  if (!p || bytes < need)
+    return fail(CQSA_ERR_INVALID_ARG, what + "the workspace has " + std::to_string(p ? bytes : 0) +
+                                          " bytes, the call needs " + std::to_string(need));
+  if (reinterpret_cast<uintptr_t>(p) % 16 != 0)
+    return fail(CQSA_ERR_INVALID_ARG, what + "the workspace must be 16-byte aligned");
+  return CQSA_OK;
+}
+
 // No range of `written` may meet another of them, or one of `read`.
 inline cqsa_status check_apart(std::initializer_list<Range> written, std::initializer_list<Range> read,
                                const std::string& what) {
