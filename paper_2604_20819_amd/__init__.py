@@ -751,9 +751,8 @@ def _ints(t, name, shape, device):
     """The address of an int32 array, or None."""
     if t is None:
         return None
-    _device_array(t, name, shape)
-    if t.device != device:
-        raise ValueError("all tensors of a call must live on one device")
+    if t.dtype != _torch().int32 or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {device}")
     return t.data_ptr()
 
 
@@ -860,13 +859,15 @@ def cqsa_draft_verify(target, draft, tokens, u, out, n_out, counts=None, lengths
     B, K = target.shape[0], target.shape[1] - 1
     if u.dtype != _torch().float32 or u.device != device or not u.is_contiguous() or u.shape != (B, K + 1):
         raise ValueError(f"u must be a contiguous float32 tensor of shape {(B, K + 1)} on {device}")
-    arrays = [_ints(t, name, shape, device) for t, name, shape in (
-        (tokens, "tokens", (B, K)), (counts, "counts", (B,)), (out, "out", (B, K + 1)), (n_out, "n_out", (B,)),
-        (lengths, "lengths", (B,)), (new_lengths, "new_lengths", (B,)))]
+    one, few = (B,), (B, K + 1)
+    tokens, counts = _ints(tokens, "tokens", (B, K), device), _ints(counts, "counts", one, device)
+    out, n_out = _ints(out, "out", few, device), _ints(n_out, "n_out", one, device)
+    lengths, new_lengths = _ints(lengths, "lengths", one, device), _ints(new_lengths, "new_lengths", one, device)
     if workspace is None:
         workspace = _workspace_on(stream, device, cqsa_draft_verify_workspace, target)
     space, size = _place(workspace, device)
-    _enqueue("cqsa_draft_verify", device, stream, p, q, arrays[0], arrays[1], u.data_ptr(), *arrays[2:], space, size)
+    _enqueue("cqsa_draft_verify", device, stream, p, q, tokens, counts, u.data_ptr(), out, n_out, lengths, new_lengths,
+             space, size)
 
 
 def cqsa_set_timing(enable):

@@ -17,11 +17,18 @@ struct VerifyArgs {
   const int32_t* lengths;
   int32_t* new_lengths;
   int32_t B, K, V;
-  void* sums;  // workspace of verify_bytes
+  int32_t len, pieces;  // VerifyPlan's
+  double* sums;         // with split: [B, pieces], then where each sequence stops, int [B]
 };
 
-uint64_t verify_bytes(int64_t B, int64_t V, cqsa_dtype dt);
+// How a call's vocabulary is divided; by its sizes alone.
+struct VerifyPlan {
+  bool split;           // work groups of their own sum the pieces
+  int32_t len, pieces;  // elements of a piece, whole loads of a wave
+  uint64_t bytes;       // of the workspace
+};
+VerifyPlan plan_verify(int64_t B, int64_t V, cqsa_dtype dt);
 
-hipError_t launch_verify(cqsa_dtype dt, const VerifyArgs& a, hipStream_t s);
+hipError_t launch_verify(cqsa_dtype dt, const VerifyArgs& a, bool split, hipStream_t s);
 
 }  // namespace cqsa

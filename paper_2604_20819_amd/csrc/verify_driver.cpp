@@ -60,12 +60,12 @@ cqsa_status verify_impl(const cqsa_probs* p, const cqsa_probs* q, const int32_t*
                         (const void*)lengths, (const void*)new_lengths})
     if (reinterpret_cast<uintptr_t>(x) % 4 != 0)
       return fail(CQSA_ERR_INVALID_ARG, what + "the arrays must be 4-byte aligned");
-  const uint64_t need = verify_bytes(p->B, p->V, p->dtype);
-  if ((st = check_workspace(workspace, workspace_bytes, need, what)) != CQSA_OK) return st;
+  const VerifyPlan plan = plan_verify(p->B, p->V, p->dtype);
+  if ((st = check_workspace(workspace, workspace_bytes, plan.bytes, what)) != CQSA_OK) return st;
   const uint64_t B = uint64_t(p->B), K = uint64_t(p->N - 1);
   const Range none{"", 0, 0};
   if ((st = check_apart({range_of("out", out, 4 * B * (K + 1)), range_of("n_out", n_out, 4 * B),
-                         range_of("new_lengths", new_lengths, 4 * B), range_of("the workspace", workspace, need)},
+                         range_of("new_lengths", new_lengths, 4 * B), range_of("the workspace", workspace, plan.bytes)},
                         {probs_range("target", *p), q ? probs_range("draft", *q) : none, range_of("tokens", tokens, 4 * B * K),
                          range_of("counts", counts, 4 * B), range_of("u", u, 4 * B * (K + 1)),
                          lengths == new_lengths ? none : range_of("lengths", lengths, 4 * B)},
@@ -90,8 +90,10 @@ cqsa_status verify_impl(const cqsa_probs* p, const cqsa_probs* q, const int32_t*
   a.B = int32_t(p->B);
   a.K = int32_t(K);
   a.V = int32_t(p->V);
-  a.sums = workspace;
-  CQSA_HIP(launch_verify(p->dtype, a, s));
+  a.len = plan.len;
+  a.pieces = plan.pieces;
+  a.sums = (double*)workspace;
+  CQSA_HIP(launch_verify(p->dtype, a, plan.split, s));
   return CQSA_OK;
 }
 
@@ -100,7 +102,7 @@ cqsa_status workspace_impl(const cqsa_probs* p, uint64_t* bytes) {
   if (!bytes) return fail(CQSA_ERR_INVALID_ARG, what + "bytes is NULL");
   *bytes = 0;
   const cqsa_status st = check_target(p, what);
-  if (st == CQSA_OK) *bytes = verify_bytes(p->B, p->V, p->dtype);
+  if (st == CQSA_OK && p->B > 0) *bytes = plan_verify(p->B, p->V, p->dtype).bytes;
   return st;
 }
 
