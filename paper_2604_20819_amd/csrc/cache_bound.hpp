@@ -27,14 +27,15 @@ struct WeighArgs {
 
 // How a call's rows and tokens are spread over work groups; by its sizes alone.
 struct WeighPlan {
-  bool many;       // the kernel for many rows
-  int row_groups;  // else groups of 16 rows
+  int row_groups;  // of 16 rows, in registers; 0: the kernel for many rows
+  bool resident;   // which holds them all in LDS
+  int waves;       // of a work group
   int tiles;       // work groups over a sequence's tokens
-  int splits;      // and, with many rows, over its rows
+  int splits;      // and over its rows
   int64_t groups;  // work groups in all
 };
-// rows: the most that a sequence and key head has.
-WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
+// rows: the most that a sequence and key head has, of `tokens` tokens.
+WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t tokens, int64_t max_len, cqsa_dtype dt, int d);
 
 // The key at which a head's kept tokens end.
 struct EvictBorder {

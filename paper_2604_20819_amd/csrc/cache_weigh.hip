@@ -56,10 +56,11 @@ __global__ void __launch_bounds__(256, (weigh_few_waves(RowType<T>::kQuery, DB, 
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int id = blockIdx.x;
+  int id = (blockIdx.y << kGridLog2) + blockIdx.x;
   const int h = id % c.H;
   id /= c.H;
   const int b = id % c.B, part = id / c.B;
+  if (part >= per_seq) return;  // behind the last work group, where the grid has two dimensions
   const Seq s = sequence(c, b);
   const int t1 = (s.len + 31) >> 5, step = 4 * per_seq;
   int t = 4 * part + wave;
@@ -192,9 +193,12 @@ __global__ void __launch_bounds__(256, (weigh_few_waves(RowType<T>::kQuery, DB, 
 
 // Many rows: a wave keeps 64 tokens' decoded keys in registers, and the work
 // group's waves go through the rows together, stage by stage of RS through LDS,
-// where a matrix operand lies as the 64 lanes read it.
-template <typename T, int DB, int W, int RS>
-__global__ void __launch_bounds__(64 * W, 2) cache_weigh_many(const WeighArgs a, int token_tiles, int splits) {
+// where a matrix operand lies as the 64 lanes read it.  RESIDENT: all rows fit the two
+// stages that LDS holds; they are brought once, and the work group goes on to every
+// `tiles`-th of its sequence's 64 W tokens, the next ones' keys on their way.
+template <typename T, int DB, int W, int RS, bool RESIDENT>
+__global__ void __launch_bounds__(64 * W, W > 8 ? 4 : sizeof(T) == 4 && W == 4 && DB > 6 ? 1 : 2)
+    cache_weigh_many(const WeighArgs a, int tiles, int splits) {
   constexpr int D = 32 * DB, QP = RowType<T>::kQuery, NT = 64 * W, TOKENS = 64 * W;
   constexpr int UNITS = RS * 4 * DB, NU = (UNITS + NT - 1) / NT;  // of 8 elements
   __shared__ __attribute__((aligned(16))) char lds[2][RS * D * 2 * QP];
@@ -203,47 +207,61 @@ __global__ void __launch_bounds__(64 * W, 2) cache_weigh_many(const WeighArgs a,
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int id = blockIdx.x;
+  int id = (blockIdx.y << kGridLog2) + blockIdx.x;
   const int h = id % c.H;
   id /= c.H;
   const int b = id % c.B;
   id /= c.B;
-  const int sp = id % splits, first = id / splits * TOKENS;
+  const int sp = id % splits, tile = id / splits, first = tile * TOKENS;
+  if (tile >= tiles) return;  // behind the last work group, where the grid has two dimensions
   const Seq s = sequence(c, b);
   if (first >= s.len) return;
   const int rows = rows_of(a, s, b), old = s.len - s.n, G = a.G;
   const int64_t tb = c.q_start ? 0 : b;
 
   // the work group's stages: those whose rows see its first token, an equal part of them
-  int begin = a.causal && first > old ? (first - old) * G / RS : 0;
+  int begin = !RESIDENT && a.causal && first > old ? (first - old) * G / RS : 0;
   const int all = (rows + RS - 1) / RS;
   const int each = all > begin ? (all - begin + splits - 1) / splits : 0;
   begin += sp * each;
   const int end = begin + each < all ? begin + each : all;
 
   // keys: half the lanes hold elements 0 .. 15 of a block, the others 16 .. 31
-  const int tok0 = first + 64 * wave;
-  bf16x8 kk[2][DB][2];
+  int tok0 = first + 64 * wave;
+  u32x2 code[2][DB];
+  uint32_t power[2][DB];
   bool there[2];
+  float had = 0.f;
+  auto fetch = [&](int t0) {
 #pragma unroll
-  for (int v = 0; v < 2; ++v) {
-    const int t = (tok0 >> 5) + v;
-    const int64_t page = 32 * t < s.len ? page_of(c, b, t) : -1;
-    there[v] = page >= 0;
-    const char* p = c.data + tile_at(c, page < 0 ? 0 : page, h, t);
-    const int key = lane & 31;
+    for (int v = 0; v < 2; ++v) {
+      const int t = (t0 >> 5) + v, key = lane & 31;
+      const int64_t page = 32 * t < s.len ? page_of(c, b, t) : -1;
+      there[v] = page >= 0;
+      const char* p = c.data + tile_at(c, page < 0 ? 0 : page, h, t);
 #pragma unroll
-    for (int w = 0; w < DB; ++w) {
-      u32x2 x = {0u, 0u};
-      uint32_t e = 0;
-      if (there[v]) {
-        x = *(const u32x2*)(p + w * 512 + key * 16 + 8 * half);
-        e = *(const uint8_t*)(p + k_exp_at(D, key, w));
+      for (int w = 0; w < DB; ++w) {
+        code[v][w] = u32x2{0u, 0u};
+        power[v][w] = 0;
+        if (there[v]) {
+          code[v][w] = *(const u32x2*)(p + w * 512 + key * 16 + 8 * half);
+          power[v][w] = *(const uint8_t*)(p + k_exp_at(D, key, w));
+        }
       }
-      kk[v][w][0] = decode8(x[0], scale_of(e, 0));
-      kk[v][w][1] = decode8(x[1], scale_of(e, 0));
     }
-  }
+    const int tok = t0 + lane;
+    had = splits == 1 && a.prior.p && tok < old ? a.prior.p[b * a.prior.b + h * a.prior.h + tok] : 0.f;
+  };
+  bf16x8 kk[2][DB][2];
+  auto decode = [&]() {
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+      for (int w = 0; w < DB; ++w)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) kk[v][w][st] = decode8(code[v][w][st], scale_of(power[v][w], 0));
+  };
+  fetch(tok0);
 
   // Rows on their way: unit u is chunk u / 16 % 4 of a block of row u % 16 of 16,
   // so that neighbouring lanes write neighbouring 16 bytes of LDS.
@@ -353,8 +371,48 @@ __global__ void __launch_bounds__(64 * W, 2) cache_weigh_many(const WeighArgs a,
     }
   };
 
+  auto finish = [&](bool there0, bool there1, float before) {
+    // the halves' lanes exchange: the lower half gets the first 32 tokens' sums
+    if (!there0) sum[0] = 0.f;
+    if (!there1) sum[1] = 0.f;
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, sum[0]),
+                                                    __builtin_bit_cast(uint32_t, sum[1]), false, false);
+    const uint32_t lo = r[0], hi = r[1];
+    const float y = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+    const int tok = tok0 + lane;
+    if (tok >= s.len) return;
+    if (splits > 1)
+      a.part[(int64_t(sp) * c.B + b) * c.H * c.max_len + int64_t(h) * c.max_len + tok] = y;
+    else
+      a.w.p[b * a.w.b + h * a.w.h + tok] = __builtin_fmaf(a.decay, before, y);
+  };
+
+  if (begin < end) load(begin);
+  if constexpr (RESIDENT) {
+    if (begin < end) put(0);
+    if (begin + 1 < end) {
+      load(begin + 1);
+      put(1);
+    }
+    __syncthreads();
+    while (tok0 < s.len) {
+      decode();
+      const bool there0 = there[0], there1 = there[1];
+      const float before = had;
+      const int next = tok0 + tiles * TOKENS;
+      if (next < s.len) fetch(next);
+      sum[0] = sum[1] = 0.f;
+      if (there0 || there1) {
+        if (begin < end) compute(0);
+        if (begin + 1 < end) compute(1);
+      }
+      finish(there0, there1, before);
+      tok0 = next;
+    }
+    return;
+  }
+  decode();
   if (begin < end) {
-    load(begin);
     put(0);
     if (begin + 1 < end) load(begin + 1);
   }
@@ -367,22 +425,7 @@ __global__ void __launch_bounds__(64 * W, 2) cache_weigh_many(const WeighArgs a,
       if (stage + 2 < end) load(stage + 2);
     }
   }
-
-  // the halves' lanes exchange: the lower half gets the first 32 tokens' sums
-  if (!there[0]) sum[0] = 0.f;
-  if (!there[1]) sum[1] = 0.f;
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, sum[0]),
-                                                  __builtin_bit_cast(uint32_t, sum[1]), false, false);
-  const uint32_t lo = r[0], hi = r[1];
-  const float y = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
-  const int tok = tok0 + lane;
-  if (tok >= s.len) return;
-  if (splits > 1) {
-    a.part[(int64_t(sp) * c.B + b) * c.H * c.max_len + int64_t(h) * c.max_len + tok] = y;
-    return;
-  }
-  const float had = a.prior.p && tok < old ? a.prior.p[b * a.prior.b + h * a.prior.h + tok] : 0.f;
-  a.w.p[b * a.w.b + h * a.w.h + tok] = __builtin_fmaf(a.decay, had, y);
+  finish(there[0], there[1], had);
 }
 
 // Adds the parts of a split call, in their order.
@@ -403,19 +446,29 @@ namespace {
 
 // Rows of a stage, so that two of them fit LDS.
 constexpr int stage_rows(int parts, int db) { return parts * db <= 8 ? 64 : 32; }
-constexpr int kManyWaves = 8;
+// Waves of a work group over long contexts, which go through more rows a byte of LDS the more
+// they are, as many as the registers of their keys allow (4096 rows of 4 heads over 32768 tokens,
+// bf16: d = 128 478 us, with 8 waves 560, with 4 554; d = 64 355, 350 and 358; d = 256, 2048
+// rows, 449 with 8, 564 with 4), and over short ones, which more work groups share more evenly
+// (4 sequences of 2000, d = 128, 89; with 16 129).
+constexpr int kShortWaves = 4;
+constexpr int long_waves(int db) { return db <= 4 ? 16 : 8; }
 
 template <typename T, int DB>
 void launch_d(const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
-  constexpr int QP = RowType<T>::kQuery, NQ = weigh_few_groups(QP, DB);
-  const dim3 grid(unsigned(p.groups));
-  if (p.many) {
-    hipLaunchKernelGGL((cache_weigh_many<T, DB, kManyWaves, stage_rows(QP, DB)>), grid, dim3(64 * kManyWaves), 0, s, a,
-                       p.tiles, p.splits);
+  constexpr int QP = RowType<T>::kQuery, NQ = weigh_few_groups(QP, DB), RS = stage_rows(QP, DB), LW = long_waves(DB);
+  const dim3 grid = attend_grid(p.groups), block(64 * p.waves);
+  if (p.row_groups == 0) {
+    if (p.resident)
+      hipLaunchKernelGGL((cache_weigh_many<T, DB, kShortWaves, RS, true>), grid, block, 0, s, a, p.tiles, 1);
+    else if (p.waves == LW)
+      hipLaunchKernelGGL((cache_weigh_many<T, DB, LW, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
+    else
+      hipLaunchKernelGGL((cache_weigh_many<T, DB, kShortWaves, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
   } else if (p.row_groups == 1) {
-    hipLaunchKernelGGL((cache_weigh_few<T, DB, 1>), grid, dim3(256), 0, s, a, p.tiles);
+    hipLaunchKernelGGL((cache_weigh_few<T, DB, 1>), grid, block, 0, s, a, p.tiles);
   } else if constexpr (NQ == 2) {
-    hipLaunchKernelGGL((cache_weigh_few<T, DB, 2>), grid, dim3(256), 0, s, a, p.tiles);
+    hipLaunchKernelGGL((cache_weigh_few<T, DB, 2>), grid, block, 0, s, a, p.tiles);
   }
 }
 
@@ -446,32 +499,49 @@ hipError_t launch_rows(const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
 
 }  // namespace
 
-WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d) {
+WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t tokens, int64_t max_len, cqsa_dtype dt, int d) {
   WeighPlan p{};
-  const int parts = dt == CQSA_F32 ? 3 : (dt == CQSA_F16 ? 2 : 1), db = d / 32;
+  const int parts = dt == CQSA_F32 ? 3 : (dt == CQSA_F16 ? 2 : 1), db = d / 32, stage = stage_rows(parts, db);
   const int64_t heads = B * H;
   p.splits = 1;
-  p.many = rows > 16 * weigh_few_groups(parts, db);
-  if (p.many) {
-    const int64_t stages = (rows + stage_rows(parts, db) - 1) / stage_rows(parts, db);
-    p.tiles = int((max_len + 64 * kManyWaves - 1) / (64 * kManyWaves));
-    const int64_t groups = heads * p.tiles;
-    p.splits = int(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(stages / 2, 64), 512 / groups)));
-    p.groups = groups * p.splits;
+  p.waves = 4;
+  if (rows <= 16 * weigh_few_groups(parts, db)) {
+    p.row_groups = rows > 16 ? 2 : 1;
+    // Work groups a sequence and head: as many as the GPU holds at once, or of several
+    // sequences, whose lengths differ, one for every 8 tiles of its waves with one group
+    // of rows and 16 with two, so that the long ones' parts even out (64 of up to
+    // 16384 tokens, 8 heads, d = 128: 67 us, with as many as fit 81; 16 of them 20 and 20;
+    // one of 2^20 126, in parts of 8 tiles 138; 64 of up to 16384, two groups of rows, 98 and 101).
+    const int64_t tiles = (max_len + 31) / 32, most = (tiles + 3) / 4;
+    const int held = parts * db * p.row_groups;
+    const int64_t fit = (held <= 4 ? 1536 : held <= 12 ? 1024 : 768) / heads;
+    const int64_t even = B == 1 ? 0 : tiles / (32 * p.row_groups);
+    p.tiles = int(std::max<int64_t>(1, std::min(most, std::max(fit, even))));
+    p.groups = heads * p.tiles;
     return p;
   }
-  p.row_groups = rows > 16 ? 2 : 1;
-  // Work groups a sequence and head: as many as the GPU holds at once, or of several
-  // sequences, whose lengths differ, one for every 8 tiles of its waves with one group
-  // of rows and 16 with two, so that the long ones' parts even out (64 of up to
-  // 16384 tokens, 8 heads, d = 128: 67 us, with as many as fit 81; 16 of them 20 and 20;
-  // one of 2^20 126, in parts of 8 tiles 138; 64 of up to 16384, two groups of rows, 98 and 101).
-  const int64_t tiles = (max_len + 31) / 32, most = (tiles + 3) / 4;
-  const int held = parts * db * p.row_groups;
-  const int64_t fit = (held <= 4 ? 1536 : held <= 12 ? 1024 : 768) / heads;
-  const int64_t even = B == 1 ? 0 : tiles / (32 * p.row_groups);
-  p.tiles = int(std::max<int64_t>(1, std::min(most, std::max(fit, even))));
-  p.groups = heads * p.tiles;
+  if (rows <= 2 * stage) {
+    // the same with tiles of 256 tokens, 4 a work group (48 rows, 64 sequences of up to 8192
+    // tokens, d = 128: 67 us, one 100; 128 rows, 16 of them 37 and 48)
+    p.resident = true;
+    const int64_t most = (max_len + 255) / 256;
+    p.tiles = int(std::max<int64_t>(1, std::min(most, std::max<int64_t>(1536 / heads, B == 1 ? 0 : most / 4))));
+    p.groups = heads * p.tiles;
+    return p;
+  }
+  // Long: most tokens were there before the rows, so that the waves of a work group all have rows.
+  const bool far = max_len >= 8192 && max_len >= 2 * tokens;
+  if (db <= 4 ? far : max_len > 1536 && dt != CQSA_F32) p.waves = long_waves(db);
+  p.tiles = int((max_len + 64 * p.waves - 1) / (64 * p.waves));
+  // The rows are split until the GPU has 8 work groups of 4 waves a CU, which evens out what causal
+  // masks leave of them (32 sequences of 300 tokens and rows of 4 heads, d = 128: 31 us in 3 or 4 parts,
+  // 54 in one; 4 of 2000 89 in 8, 159 in 2), or as many as their registers allow (d = 256: 32 of 300
+  // 56 in 2, 61 in 3; fp32, 2 of 1000 94 in 8, 118 in 24), or 2 of more waves; of 128 rows at least.
+  const int64_t groups = heads * p.tiles;
+  const int64_t total = p.waves > 4 || (db > 4 && dt == CQSA_F32) ? 512 : db > 4 ? 1024 : 2048;
+  const int64_t most = std::min<int64_t>(rows / 128, 64);
+  p.splits = int(std::max<int64_t>(1, std::min(most, (total + groups - 1) / groups)));
+  p.groups = groups * p.splits;
   return p;
 }
 
