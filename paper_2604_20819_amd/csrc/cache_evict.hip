@@ -17,7 +17,7 @@ namespace cqsa {
 namespace {
 
 constexpr uint32_t kForced = 0xffffffffu;
-constexpr int kItems = 16;    // keys of a lane
+constexpr int kItems = 16;    // keys of a lane of a work group that shares a head with others
 constexpr int kBins = 2048;   // of a digit
 constexpr int kChunk = 4096;  // tokens of a work group that shares a head with others
 // words of a head in memory: three digits' counts, and how many tokens have no page
@@ -36,22 +36,35 @@ __device__ __forceinline__ int length_of(const CacheArgs& c, int b) {
   return n < 0 ? 0 : (n > c.max_len ? c.max_len : n);
 }
 
-// Keys of the wave's tokens t0 + 64 i + lane; behind the sequence 0.
-__device__ __forceinline__ void load_keys(const EvictArgs& a, const float* w, int b, int len, int t0, int lane,
-                                          uint32_t* key) {
-  float x[kItems];
-  int32_t page[kItems];
+// The key of token t, by its weight and its page (-1 behind the sequence).
+__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, float w, int32_t page, int t, int len) {
+  const uint32_t k = t < a.first || t >= len - a.recent ? kForced : rank_of(w);
+  return page < 0 || page >= a.c.n_pages ? 0u : k;
+}
+
+// Keys of a wave's tokens t0 + step i + lane, i < items, by use(i, key).  A work group goes through its code
+// once, so that long code costs more than it does: 8 loads at a time, and keys that are looked at
+// again lie in LDS.
+template <typename F>
+__device__ __forceinline__ void each_key(const EvictArgs& a, const float* w, int b, int len, int t0, int step, int items,
+                                         F use) {
+  constexpr int U = 8;
+#pragma unroll 1
+  for (int i0 = 0; i0 < items; i0 += U) {
+    float x[U];
+    int32_t page[U];
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    const int t = t0 + 64 * i + lane;
-    x[i] = t < len ? w[t] : 0.f;
-    page[i] = t < len ? a.c.pages[b * a.c.pages_stride + (t >> a.c.page_log2)] : -1;
-  }
+    for (int k = 0; k < U; ++k) {
+      const int t = t0 + step * (i0 + k);
+      const bool here = i0 + k < items && t < len;
+      x[k] = here ? w[t] : 0.f;
+      page[k] = here ? a.c.pages[b * a.c.pages_stride + (t >> a.c.page_log2)] : -1;
+    }
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    const int t = t0 + 64 * i + lane;
-    const bool forced = t < a.first || t >= len - a.recent;
-    key[i] = page[i] < 0 || page[i] >= a.c.n_pages ? 0u : forced ? kForced : rank_of(x[i]);
+    for (int k = 0; k < U; ++k) {
+      if (i0 + k >= items) break;
+      use(i0 + k, key_of(a, x[k], page[k], t0 + step * (i0 + k), len));
+    }
   }
 }
 
@@ -100,32 +113,38 @@ __device__ __forceinline__ EvictBorder next_digit(const uint32_t* count, const E
   return next;
 }
 
-// Places of a wave's kept keys: above the border, or among the first `left` that equal it,
-// with n0 and n1 such keys before the wave's.
-__device__ __forceinline__ void place(const uint32_t* key, const EvictBorder& at, int t0, int lane, int n0, int n1,
-                                      int32_t* kept) {
-  const uint64_t below = (uint64_t(1) << lane) - 1;
-#pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    const uint64_t above = __builtin_amdgcn_ballot_w64(key[i] > at.key);
-    const uint64_t equal = __builtin_amdgcn_ballot_w64(key[i] == at.key);
-    const int m0 = n0 + __builtin_popcountll(above & below), m1 = n1 + __builtin_popcountll(equal & below);
-    if (key[i] > at.key)
-      kept[m0 + (m1 < at.left ? m1 : at.left)] = t0 + 64 * i + lane;
-    else if (key[i] == at.key && m1 < at.left)
-      kept[m0 + m1] = t0 + 64 * i + lane;
-    n0 += __builtin_popcountll(above), n1 += __builtin_popcountll(equal);
-  }
+__device__ __forceinline__ int lanes_below(uint64_t m) {
+  return int(__builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), 0u)));
 }
 
-__device__ __forceinline__ void count_keys(const uint32_t* key, const EvictBorder& at, int* n0, int* n1) {
-  *n0 = *n1 = 0;
-#pragma unroll
-  for (int i = 0; i < kItems; ++i) {
-    *n0 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] > at.key));
-    *n1 += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] == at.key));
-  }
+// Adds a key to its digit's count in LDS where it shares the border's upper ones.  Zeros, of which there
+// may be very many, are counted by themselves and added once (512 heads of 16384 of them: 102 us with an
+// addition each, which one address takes one after the other).
+constexpr uint32_t kZero = 0x80000000u;
+__device__ __forceinline__ void count_key(uint32_t* count, uint32_t k, const EvictBorder& at, int pass) {
+  if (k != 0u && k != kZero && shares(k, at.key, pass)) atomicAdd(&count[digit_of(k, pass)], 1u);
 }
+__device__ __forceinline__ void count_zeros(uint32_t* count, int zeros, const EvictBorder& at, int pass) {
+  if (zeros > 0 && shares(kZero, at.key, pass)) atomicAdd(&count[digit_of(kZero, pass)], uint32_t(zeros));
+}
+__device__ __forceinline__ int lanes_of(bool x) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(x)); }
+
+// Places of 64 keys in a row, a lane each: kept are those above the border, and the first `left` that equal
+// it; n0 and n1 such keys lie before them.
+__device__ __forceinline__ void place(uint32_t k, const EvictBorder& at, int t, int n0, int n1, int32_t* kept) {
+  const uint64_t above = __builtin_amdgcn_ballot_w64(k > at.key), equal = __builtin_amdgcn_ballot_w64(k == at.key);
+  const int m0 = n0 + lanes_below(above), m1 = n1 + lanes_below(equal);
+  if (k > at.key || (k == at.key && m1 < at.left)) kept[m0 + (m1 < at.left ? m1 : at.left)] = t;
+}
+
+// A wave's keys above the border, and those that equal it.
+struct Counts {
+  int above, equal;
+  __device__ __forceinline__ void add(uint32_t k, const EvictBorder& at) {
+    above += lanes_of(k > at.key);
+    equal += lanes_of(k == at.key);
+  }
+};
 
 constexpr EvictBorder kNothing = {kForced, 0};  // of a sequence that keeps nothing
 
@@ -133,10 +152,11 @@ __device__ __forceinline__ int kept_of(const EvictArgs& a, int present) { return
 
 }  // namespace
 
-// A work group of WAVES takes all of a head's tokens, 1024 a wave.
-template <int WAVES>
-__global__ void __launch_bounds__(64 * WAVES) cache_evict_select(const EvictArgs a) {
-  constexpr int NT = 64 * WAVES;
+// A work group takes all of a head's tokens, 16 waves of 64 ITEMS in a row, whose keys stay in registers.
+// What bounds it is issuing the 100 instructions or so that 64 keys cost in all.
+template <int ITEMS>
+__global__ void __launch_bounds__(1024, 8) cache_evict_select(const EvictArgs a) {
+  constexpr int WAVES = 16, NT = 64 * WAVES;
   __shared__ uint32_t count[kBins];
   __shared__ int scratch[WAVES + 2];
   __shared__ int before[2][WAVES];
@@ -147,41 +167,74 @@ __global__ void __launch_bounds__(64 * WAVES) cache_evict_select(const EvictArgs
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = length_of(a.c, b);
   const float* w = a.w.p + b * a.w.b + h * a.w.h;
-  const int t0 = 1024 * wave;
-  uint32_t key[kItems];
-  load_keys(a, w, b, len, t0, lane, key);
-  int present = 0;
+  const int t0 = 64 * ITEMS * wave;
+  const bool some = t0 < len;  // waves without tokens pass the code by
+  for (int i = tid; i < kBins; i += NT) count[i] = 0;
+  uint32_t key[ITEMS];
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) present += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] != 0u));
-  if (lane == 0) before[0][wave] = present;
-  EvictBorder at = {0u, 0};
-  for (int pass = 0; pass < 3; ++pass) {
-    for (int i = tid; i < kBins; i += NT) count[i] = 0;
-    __syncthreads();
-    if (pass == 0) {
-      present = 0;
+  for (int i = 0; i < ITEMS; ++i) key[i] = 0u;
+  int present = 0, zeros = 0;
+  if (some) {
+    constexpr int U = ITEMS < 8 ? ITEMS : 8;  // loads at a time
 #pragma unroll
-      for (int i = 0; i < WAVES; ++i) present += before[0][i];
-      at.left = kept_of(a, present);
-      if (at.left == 0) break;
+    for (int i0 = 0; i0 < ITEMS; i0 += U) {
+      float x[U];
+      int32_t page[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int t = t0 + 64 * (i0 + i) + lane;
+        x[i] = t < len ? w[t] : 0.f;
+        page[i] = t < len ? a.c.pages[b * a.c.pages_stride + (t >> a.c.page_log2)] : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) key[i0 + i] = key_of(a, x[i], page[i], t0 + 64 * (i0 + i) + lane, len);
     }
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      if (key[i] != 0u && shares(key[i], at.key, pass)) atomicAdd(&count[digit_of(key[i], pass)], 1u);
-    __syncthreads();
-    at = next_digit<NT>(count, at, pass, scratch);
+    for (int i = 0; i < ITEMS; ++i) present += lanes_of(key[i] != 0u), zeros += lanes_of(key[i] == kZero);
   }
+  if (lane == 0) before[0][wave] = present;
+  __syncthreads();
+  present = 0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) present += before[0][i];
   const int keep = kept_of(a, present);
-  if (keep == 0) at = kNothing;
-  int n0, n1;
-  count_keys(key, at, &n0, &n1);
+  EvictBorder at = {0u, keep};
+  if (keep == 0) {
+    at = kNothing;
+  } else {
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      if (pass > 0) {
+        for (int i = tid; i < kBins; i += NT) count[i] = 0;
+        __syncthreads();
+      }
+      if (some) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) count_key(count, key[i], at, pass);
+      }
+      if (lane == 0) count_zeros(count, zeros, at, pass);
+      __syncthreads();
+      at = next_digit<NT>(count, at, pass, scratch);
+    }
+  }
+  Counts n = {0, 0};
+  if (some) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) n.add(key[i], at);
+  }
   __syncthreads();
-  if (lane == 0) before[0][wave] = n0, before[1][wave] = n1;
+  if (lane == 0) before[0][wave] = n.above, before[1][wave] = n.equal;
   __syncthreads();
-  n0 = n1 = 0;
+  int n0 = 0, n1 = 0;
   for (int i = 0; i < wave; ++i) n0 += before[0][i], n1 += before[1][i];
   int32_t* kept = a.kept + id * a.kept_stride;
-  place(key, at, t0, lane, n0, n1, kept);
+  if (some) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      place(key[i], at, t0 + 64 * i + lane, n0, n1, kept);
+      n0 += lanes_of(key[i] > at.key), n1 += lanes_of(key[i] == at.key);
+    }
+  }
   if (a.pad)
     for (int i = keep + tid; i < a.budget; i += NT) kept[i] = -1;
   if (h == 0 && tid == 0) a.n_kept[b] = keep;
@@ -233,34 +286,31 @@ __global__ void __launch_bounds__(256) cache_evict_count(const EvictArgs a, int 
     for (int i = tid; i < kBins; i += 256) count[i] = 0;
     __syncthreads();
   }
-  int absent = 0;
+  int absent = 0, zeros = 0;
   for (int chunk = part; chunk < a.chunks; chunk += per) {
     const int t0 = chunk * kChunk + 1024 * wave;
-    uint32_t key[kItems];
-    int n0 = 0, n1 = 0;
-    if (t0 < len) {
-      load_keys(a, w, b, len, t0, lane, key);
+    const int items = t0 < len ? kItems : 0;
+    Counts n = {0, 0};
+    each_key(a, w, b, len, t0 + lane, 64, items, [&](int i, uint32_t k) {
       if (PASS == 3) {
-        count_keys(key, at, &n0, &n1);
+        n.add(k, at);
       } else {
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-          if (PASS == 0) absent += key[i] == 0u && t0 + 64 * i + lane < len;
-          if (key[i] != 0u && shares(key[i], at.key, PASS)) atomicAdd(&count[digit_of(key[i], PASS)], 1u);
-        }
+        if (PASS == 0) absent += k == 0u && t0 + 64 * i + lane < len;
+        zeros += lanes_of(k == kZero);
+        count_key(count, k, at, PASS);
       }
-    }
+    });
     if (PASS == 3) {
       __syncthreads();
-      if (lane == 0) scratch[wave] = n0, count[wave] = uint32_t(n1);
+      if (lane == 0) scratch[wave] = n.above, count[wave] = uint32_t(n.equal);
       __syncthreads();
-      if (tid == 0) {
+      if (tid == 0)
         a.chunk_counts[id * a.chunks + chunk] =
             int2{scratch[0] + scratch[1] + scratch[2] + scratch[3], int(count[0] + count[1] + count[2] + count[3])};
-      }
     }
   }
   if (PASS == 3) return;
+  if (lane == 0) count_zeros(count, zeros, at, PASS);
   if (PASS == 0 && absent) atomicAdd(&words[3 * kBins], uint32_t(absent));
   __syncthreads();
   for (int i = tid; i < kBins; i += 256)
@@ -268,6 +318,7 @@ __global__ void __launch_bounds__(256) cache_evict_count(const EvictArgs a, int 
 }
 
 __global__ void __launch_bounds__(256) cache_evict_place(const EvictArgs a, int per) {
+  __shared__ uint32_t keys[kChunk];
   __shared__ int before[2][4], own[2][4];
   const int64_t id = blockIdx.x / per;
   const int part = blockIdx.x % per;
@@ -283,8 +334,13 @@ __global__ void __launch_bounds__(256) cache_evict_place(const EvictArgs a, int 
   int from = 0, sum0 = 0, sum1 = 0;  // keys of the chunks before, this thread's part of them
   for (int chunk = part; int64_t(chunk) * kChunk < len; chunk += per) {
     const int t0 = chunk * kChunk + 1024 * wave;
-    uint32_t key[kItems];
-    load_keys(a, w, b, len, t0, lane, key);
+    const int items = t0 < len ? kItems : 0;
+    uint32_t* const key = keys + 1024 * wave;
+    Counts n = {0, 0};
+    each_key(a, w, b, len, t0 + lane, 64, items, [&](int i, uint32_t k) {
+      key[64 * i + lane] = k;
+      n.add(k, at);
+    });
     for (int i = from + tid; i < chunk; i += 256) {
       const int2 x = chunks[i];
       sum0 += x.x, sum1 += x.y;
@@ -293,17 +349,19 @@ __global__ void __launch_bounds__(256) cache_evict_place(const EvictArgs a, int 
     int m0 = sum0, m1 = sum1;
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) m0 += __shfl_xor(m0, k), m1 += __shfl_xor(m1, k);
-    int n0, n1;
-    count_keys(key, at, &n0, &n1);
     __syncthreads();
-    if (lane == 0) before[0][wave] = m0, before[1][wave] = m1, own[0][wave] = n0, own[1][wave] = n1;
+    if (lane == 0) before[0][wave] = m0, before[1][wave] = m1, own[0][wave] = n.above, own[1][wave] = n.equal;
     __syncthreads();
-    n0 = n1 = 0;
+    int n0 = 0, n1 = 0;
     for (int i = 0; i < 4; ++i) {
       n0 += before[0][i], n1 += before[1][i];
       if (i < wave) n0 += own[0][i], n1 += own[1][i];
     }
-    place(key, at, t0, lane, n0, n1, kept);
+    for (int i = 0; i < items; ++i) {
+      const uint32_t k = key[64 * i + lane];
+      place(k, at, t0 + 64 * i + lane, n0, n1, kept);
+      n0 += lanes_of(k > at.key), n1 += lanes_of(k == at.key);
+    }
   }
   if (a.pad)
     for (int64_t i = keep + int64_t(part) * 256 + tid; i < a.budget; i += int64_t(per) * 256) kept[i] = -1;
@@ -406,7 +464,7 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t s) {
   const int64_t heads = int64_t(a.c.B) * a.c.H;
   if (a.chunks == 0) {
     if (a.c.max_len <= 4096)
-      hipLaunchKernelGGL((cache_evict_select<4>), attend_grid(heads), dim3(256), 0, s, a);
+      hipLaunchKernelGGL((cache_evict_select<4>), attend_grid(heads), dim3(1024), 0, s, a);
     else
       hipLaunchKernelGGL((cache_evict_select<16>), attend_grid(heads), dim3(1024), 0, s, a);
   } else {

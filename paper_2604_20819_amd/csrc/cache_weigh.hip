@@ -232,6 +232,9 @@ __global__ void __launch_bounds__(64 * W, W > 8 ? 4 : sizeof(T) == 4 && W == 4 &
   uint32_t power[2][DB];
   bool there[2];
   float had = 0.f;
+  auto prior_at = [&](int tok) {
+    return a.prior.p && tok < old ? a.prior.p[b * a.prior.b + h * a.prior.h + tok] : 0.f;
+  };
   auto fetch = [&](int t0) {
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
@@ -249,8 +252,7 @@ __global__ void __launch_bounds__(64 * W, W > 8 ? 4 : sizeof(T) == 4 && W == 4 &
         }
       }
     }
-    const int tok = t0 + lane;
-    had = splits == 1 && a.prior.p && tok < old ? a.prior.p[b * a.prior.b + h * a.prior.h + tok] : 0.f;
+    if (RESIDENT) had = prior_at(t0 + lane);
   };
   bf16x8 kk[2][DB][2];
   auto decode = [&]() {
@@ -425,7 +427,7 @@ __global__ void __launch_bounds__(64 * W, W > 8 ? 4 : sizeof(T) == 4 && W == 4 &
       if (stage + 2 < end) load(stage + 2);
     }
   }
-  finish(there[0], there[1], had);
+  finish(there[0], there[1], splits == 1 ? prior_at(tok0 + lane) : 0.f);
 }
 
 // Adds the parts of a split call, in their order.
