@@ -560,7 +560,7 @@ typedef struct {
  *   W[b][h][t] = decay prior[b][h][t] + sum over i of exp(s_it - LSE_i),   0 <= t < lengths[b].
  * Q, LSE (fp32 [B, H_q, L]), causal and scale as in cqsa_cache_attend, which leaves that LSE.  prior (or
  * NULL: zeros) is read at the tokens that were there before the call's rows, t < lengths[b] - n_b; the rows'
- * own tokens start from 0 whatever it holds.  prior may be W itself, else it lies apart from it (which is
+ * own tokens start from 0 whatever it holds, and with decay = 0 all do.  prior may be W itself, else it lies apart from it (which is
  * checked).  W from lengths[b] on is left as it was.  counts: int32 [B] in device memory, or NULL: the sums
  * go over the first counts[b] rows of sequence b alone (taken into [0, n_b]), as where the other rows'
  * drafts were rejected.  Rows whose LSE is not finite (they saw nothing, or a NaN) add nothing; tokens whose
@@ -589,7 +589,7 @@ typedef struct {
  * different tokens.  Tokens whose page entry holds nothing are never kept and count for no budget (a first or recent
  * one is simply gone).  Keys keep what was written, positions turned into them among it.
  * to = NULL: in place; tokens and W move together within the sequence's pages, W_to is NULL, and bytes and
- * weights behind the kept ones stay as they were.  Else the kept tokens go to the pages of to's tables
+ * weights behind the kept ones stay as they were; a token whose new place's page holds nothing is lost.  Else the kept tokens go to the pages of to's tables
  * (its lengths, q_start and bounds are not read), which share no page with the batch's (what such a page gets is not
  * specified), and the kept tokens' weights to W_to, or nowhere where that is NULL; W stays.  Sequences share pages
  * only where the pages that are written are each one sequence's.

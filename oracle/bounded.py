@@ -34,6 +34,27 @@ def weigh(q, k, lse, there, length, count, causal, scale, prior, decay):
     return W, big
 
 
+def weigh_rows(q, k, lse, there, length, count, causal, scale, prior, decay):
+    """weigh() by matrix products, a key head at a time; every LSE finite."""
+    n, Hq, _ = q.shape
+    H = k.shape[1]
+    G = Hq // H
+    W, big = np.zeros((H, length)), np.zeros((H, length))
+    t = np.arange(length)
+    last = length - n + 1 + np.arange(n) if causal else np.full(n, length)
+    seen = (t < last[:, None]) & there[:length] & (np.arange(n) < count)[:, None]
+    for h in range(Hq):
+        kk = k[:length, h // G]
+        s = q[:, h] @ kk.T * scale
+        W[h // G] += np.where(seen, np.exp(np.where(seen, s, -np.inf) - np.maximum(lse[:, h, None], -1e300)), 0.0).sum(0)
+        size = np.maximum(np.abs(q[:, h]) @ np.abs(kk).T * scale, np.abs(lse[:, h, None]))
+        big[h // G] = np.maximum(big[h // G], np.where(seen, size, 0.0).max(0, initial=0.0))
+    old = max(0, length - n)
+    if prior is not None:
+        W[:, :old] += decay * prior[:, :old]
+    return W, big
+
+
 def keep(w, there, length, budget, first, recent):
     """The positions that a head with weights w [>= length] keeps, in order."""
     def rank(t):

@@ -285,7 +285,7 @@ cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqs
   a.q = tensor_of(*Q);
   a.lse = LSE;
   a.counts = counts;
-  a.prior = weights_of(prior);
+  a.prior = weights_of(decay > 0.f ? prior : nullptr);  // 0 of a NaN is none
   a.w = weights_of(W);
   a.Hq = int32_t(Q->H);
   a.G = int32_t(Q->H / c->H);

@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(1024, 8) cache_evict_select(const EvictArgs a)
     }
   }
   if (a.pad)
-    for (int i = keep + tid; i < a.budget; i += NT) kept[i] = -1;
+    for (int64_t i = keep + tid; i < a.budget; i += NT) kept[i] = -1;
   if (h == 0 && tid == 0) a.n_kept[b] = keep;
 }
 

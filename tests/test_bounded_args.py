@@ -263,5 +263,12 @@ def test_oracle_weigh():
     lse = np.log(np.exp(x).sum(-1))
     W, _ = ob.weigh(q, k, lse, np.ones(9, bool), 9, 3, True, 0.25, None, 1.0)
     assert W.sum(-1) == pytest.approx(6.0)
+    there = np.ones(9, bool)
+    there[4] = False
+    for causal in (True, False):
+        for count in (0, 2, 3):
+            a = ob.weigh(q, k, lse, there, 9, count, causal, 0.25, np.ones((2, 9)), 0.5)
+            b = ob.weigh_rows(q, k, lse, there, 9, count, causal, 0.25, np.ones((2, 9)), 0.5)
+            assert a[0] == pytest.approx(b[0], abs=1e-12) and a[1] == pytest.approx(b[1], abs=1e-12)
     W, _ = ob.weigh(q, k, lse, np.ones(9, bool), 9, 1, True, 0.25, np.ones((2, 9)), 0.5)
     assert W.sum(-1) == pytest.approx(2.0 + 3.0) and (W[:, 7:] == 0).all()

@@ -214,6 +214,30 @@ def test_long_sequences(n, budget, kind):
         assert torch.equal(y[0].transpose(0, 1), want)
 
 
+def test_more_sequences_and_heads_than_one_dimension_takes():
+    need_gpu()
+    say("evict many heads")
+    B, H = 32768, 65
+    cache = cq.Cache4(1, H, 32, page_size=64)
+    g = torch.Generator("cuda").manual_seed(3)
+    lengths = torch.randint(0, 33, (B,), generator=g, device="cuda", dtype=torch.int32)
+    batch = cq.CacheBatch(torch.zeros(B, 1, dtype=torch.int32, device="cuda"), lengths, max_len=32)
+    W = torch.rand(B, H, 32, generator=g, device="cuda")
+    new = torch.zeros(B, dtype=torch.int32, device="cuda")
+    kept = torch.zeros(B, H, 9, dtype=torch.int32, device="cuda")
+    W_to = torch.full((B, H, 9), 7.0, device="cuda")
+    nowhere = torch.full((B, 1), -1, dtype=torch.int32, device="cuda")
+    cq.cqsa_cache_evict(cache, batch, W, new, 9, to=nowhere, W_to=W_to, kept=kept)
+    t = torch.arange(32, device="cuda")
+    w = W.masked_fill(t >= lengths[:, None, None], -1)
+    order = torch.sort(w, dim=-1, descending=True, stable=True).indices[..., :9]
+    n = lengths.clamp(max=9)
+    gone = (torch.arange(9, device="cuda") >= n[:, None])[:, None]
+    want = order.masked_fill(gone, 99).sort(-1).values
+    assert torch.equal(new, n) and torch.equal(kept.long(), torch.where(want == 99, -1, want))
+    assert torch.equal(W_to, torch.where(gone, 7.0, W.gather(-1, want.clamp(max=31))))
+
+
 def test_strided_weights_another_stream_and_capture():
     need_gpu()
     say("evict captured")

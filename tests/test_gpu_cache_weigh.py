@@ -27,7 +27,7 @@ def attended(case, cache, batch, q, causal, scale=0.0):
     return lse
 
 
-def check(case, q, lse, W, new, counts, causal, scale, prior, decay, packed, first=0, untouched=None):
+def check(case, q, lse, W, new, counts, causal, scale, prior, decay, packed, first=0, oracle=ob.weigh):
     """Every sequence's weights against the oracle; what lies behind its tokens is untouched."""
     torch.cuda.synchronize()
     d, G = case.d, q.shape[2] // case.H
@@ -41,19 +41,19 @@ def check(case, q, lse, W, new, counts, causal, scale, prior, decay, packed, fir
         there = (page >= 0) & (page < case.n_pages)
         old = None if prior is None else prior[b].cpu().double().numpy()
         c = m if counts is None else min(max(int(counts[b]), 0), m)
-        want, big = ob.weigh(qc[bb, rows], k, lc[bb][:, rows].T, there, n, c, causal, scale, old, decay)
+        want, big = oracle(qc[bb, rows], k, lc[bb][:, rows].T, there, n, c, causal, scale, old, decay)
         got = Wc[b, :, :n]
         bound = want * HALF * ((d + 8) * big + c * G + 16) + 1e-36
         err = np.abs(got - want)
         assert np.isfinite(got).all() and (err <= bound).all(), (b, err.max(), (err / bound).max())
         worst = max(worst, (err / bound).max() if err.size else 0.0)
-        assert (Wc[b, :, n:] == (7.0 if untouched is None else untouched)).all()
+        assert (Wc[b, :, n:] == 7.0).all()
         at += m
     return worst
 
 
 def run(case, Hq, new, dtype, causal=True, counts=None, decay=1.0, with_prior=True, packed=False, scale=0.0,
-        max_len=0, first=0, spare=3, in_place=False):
+        max_len=0, first=0, spare=3, in_place=False, oracle=ob.weigh):
     g = case.g
     T = case.table.shape[1] * case.page + spare
     shape = (1, first + sum(new) + 2, Hq, case.d) if packed else (len(new), new[0], Hq, case.d)
@@ -74,7 +74,7 @@ def run(case, Hq, new, dtype, causal=True, counts=None, decay=1.0, with_prior=Tr
         W = prior
     cnt = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
     cq.cqsa_cache_weigh(cache, batch, q, lse, W, prior=prior, decay=decay, counts=cnt, causal=causal, scale=scale)
-    return check(case, q, lse, W, new, counts, causal, scale or 1 / math.sqrt(case.d), keep, decay, packed, first)
+    return check(case, q, lse, W, new, counts, causal, scale or 1 / math.sqrt(case.d), keep, decay, packed, first, oracle)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
@@ -97,6 +97,59 @@ def test_chunk(d, dtype, n, G):
     case = Case(d + n, [150, 20, 5], 2, d, 32)
     case.fill_tokens()
     run(case, 2 * G, [n] * 3, dtype, decay=0.75)
+
+
+def any_tokens(case, power=122):
+    """Fills the pool with random codes, whose powers are near 2^(power - 127)."""
+    case.data = case.g.integers(0, 256, case.data.shape, dtype=np.uint8)
+    tiles = case.data.reshape(case.n_pages, -1, 34 * case.d)
+    tiles[..., 32 * case.d:] = power + tiles[..., 32 * case.d:] % 3
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d,n,L,page", [(32, 8500, 150, 256), (96, 8200, 97, 32), (128, 8193, 140, 64), (160, 1700, 81, 128),
+                                        (256, 1801, 70, 64), (256, 900, 70, 32)])
+def test_long_contexts(d, n, L, page, dtype):
+    """Many rows over contexts for which work groups have more waves, with splits of the rows."""
+    need_gpu()
+    say("weigh long", d, n, L, dtype)
+    case = Case(n + d, [n, n // 3, L // 2], 1, d, page)
+    any_tokens(case)
+    case.table[0, 1] = -1
+    run(case, 4, [L] * 3, dtype, counts=[L, L - 7, L], decay=0.5, oracle=ob.weigh_rows if n > 1000 else ob.weigh)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 4, 5, 16, 17, 32, 33, 63, 64, 65, 127, 128, 129, 192, 257])
+def test_row_counts(rows):
+    """Around the borders between the kernels, and a kernel's own steps."""
+    need_gpu()
+    say("weigh rows", rows)
+    case = Case(rows, [700, 260, 90], 2, 64, 64)
+    any_tokens(case)
+    run(case, 2, [rows] * 3, "bf16", causal=False, oracle=ob.weigh_rows)
+    run(case, 2, [rows] * 3, "f16", causal=False, oracle=ob.weigh_rows)
+
+
+def test_more_sequences_and_heads_than_one_dimension_takes():
+    """2^21 work groups and more; every sequence has the same tokens and queries."""
+    need_gpu()
+    say("weigh many heads")
+    for L, G in ((1, 1), (20, 2)):
+        B, H = 32768, 65
+        case = Case(L, [40], H, 32, 64, extra_columns=0)
+        any_tokens(case)
+        cache = case.cache()
+        table = torch.from_numpy(case.table).cuda().expand(B, -1)
+        batch = cq.CacheBatch(table.contiguous(), torch.full((B,), 40, dtype=torch.int32, device="cuda"))
+        q = normal(case.g, (1, L, H * G, 32), "bf16").cuda().expand(B, -1, -1, -1)
+        lse = torch.zeros(B, H * G, L, device="cuda")
+        W = torch.full((B, H, 64), 7.0, device="cuda")
+        cq.cqsa_cache_weigh(cache, batch, q, lse, W)
+        one = torch.full((1, H, 64), 7.0, device="cuda")
+        cq.cqsa_cache_weigh(cache, case.batch(), q[:1].contiguous(), lse[:1].contiguous(), one)
+        check(case, q[:1], lse[:1], one, [L], None, True, 32 ** -0.5, None, 1.0, False, oracle=ob.weigh_rows)
+        # one sequence's rows may be added in another order
+        assert torch.allclose(W, one.expand(B, -1, -1), rtol=2.0 ** -18)
 
 
 @pytest.mark.parametrize("page", [32, 64, 128, 256])
@@ -135,6 +188,14 @@ def test_in_place_and_without_prior():
     run(case, 4, [3, 3], "bf16", decay=0.9, in_place=True)
     run(case, 4, [3, 3], "bf16", with_prior=False, decay=0.9)
     run(case, 4, [3, 3], "bf16", decay=0.0)
+    cache, batch = case.cache(), case.batch()
+    q = normal(case.g, (2, 3, 4, 128), "bf16").cuda()
+    lse = attended(case, cache, batch, q, True)
+    a = torch.full((2, 2, case.table.shape[1] * 64), 7.0, device="cuda")
+    b = a.clone()
+    cq.cqsa_cache_weigh(cache, batch, q, lse, a)
+    cq.cqsa_cache_weigh(cache, batch, q, lse, b, prior=torch.full_like(b, math.nan), decay=0.0)
+    assert torch.equal(a, b)  # nothing of a prior that counts for nothing
 
 
 def test_pages_that_hold_nothing():
