@@ -359,9 +359,15 @@ def cqsa_plan(L, H, d, causal, device_budget_bytes=0, opts=None):
 
 
 # ---------------------------------------------------------------- torch glue
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dtype_code(t):
@@ -469,7 +475,7 @@ def _view(t, device):
         raise ValueError("tensors must be [B, L, H, d]")
     if s[3] != 1:
         raise ValueError("the last dimension must be contiguous")
-    code = _dtypes().get(t.dtype)
+    code = (_dtype_table or _dtypes()).get(t.dtype)
     if code is None:
         raise ValueError(f"tensors must be float32, float16 or bfloat16, got {t.dtype}")
     return _VIEW.pack(t.data_ptr(), code, n[0], n[1], n[2], n[3], s[0], s[1], s[2])
@@ -500,23 +506,31 @@ def _int32(**sizes):
             raise ValueError(f"{name} must be in [0, 2^31), got {x}")
 
 
-def _raw_stream():
-    """The current stream of a device by its index, as an integer: torch's own short
-    way where it has one (it saves 1.5 us of every call), else by its stream object."""
-    torch = _torch()
-    return getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
-        (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_short = None
+
+
+def _short_calls():
+    """The current device's index and the current stream (an integer) of a device by its index: torch's
+    own short ways where it has them (they save 2 us of every call), else by its objects."""
+    global _short
+    if _short is None:
+        torch = _torch()
+        _short = (getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device,
+                  getattr(torch._C, "_cuda_getCurrentRawStream", None) or
+                  (lambda i: torch.cuda.current_stream(i).cuda_stream))
+    return _short
 
 
 def _enqueue(name, device, stream, *args):
     """The call `name` with `device` current, on `stream` or the device's current one."""
-    cuda = _torch().cuda
-    if device.index != cuda.current_device():
-        with cuda.device(device):
+    current_device, current_stream = _short or _short_calls()
+    index = device.index
+    if index != current_device():
+        with _torch().cuda.device(device):
             return _enqueue(name, device, stream, *args)
     if stream is None:
-        stream = _raw_stream()(device.index)
-    status = _call(name)(*args, stream)
+        stream = current_stream(index)
+    status = (_calls.get(name) or _call(name))(*args, stream)
     if status != 0:
         _check(status, name)
 
@@ -718,9 +732,9 @@ def _place(workspace, device):
 
 def _lse(LSE, Q, device):
     """The address of an LSE for the rows of Q."""
-    want = (Q.shape[0], Q.shape[2], Q.shape[1])
-    if LSE.dtype != _torch().float32 or LSE.device != device or not LSE.is_contiguous() or LSE.shape != want:
-        raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {want} on {device}")
+    B, L, H, _ = Q.shape
+    if LSE.dtype is not _torch().float32 or LSE.device != device or not LSE.is_contiguous() or LSE.shape != (B, H, L):
+        raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {(B, H, L)} on {device}")
     return LSE.data_ptr()
 
 
@@ -742,16 +756,16 @@ def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, work
 def _weights(t, name, device):
     """The bytes of t's cqsa_weights."""
     s, n = t.stride(), t.shape
-    if t.dtype != _torch().float32 or t.device != device or len(s) != 3 or (n[2] > 1 and s[2] != 1):
+    if t.dtype is not _torch().float32 or t.device != device or len(s) != 3 or (s[2] != 1 and n[2] > 1):
         raise ValueError(f"{name} must be a float32 tensor [B, H, T] on {device} with contiguous tokens")
-    return _WEIGHTS.pack(t.data_ptr(), n[0], n[1], n[2], s[0], s[1])
+    return _WEIGHTS.pack(t.data_ptr(), *n, s[0], s[1])
 
 
 def _ints(t, name, shape, device):
     """The address of an int32 array, or None."""
     if t is None:
         return None
-    if t.dtype != _torch().int32 or t.device != device or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not _torch().int32 or t.device != device or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {device}")
     return t.data_ptr()
 
@@ -776,7 +790,7 @@ def cqsa_cache_weigh(cache, batch, Q, LSE, W, prior=None, decay=1.0, counts=None
     q, w = _view(Q, device), _weights(W, "W", device)
     old = w if prior is W else None if prior is None else _weights(prior, "prior", device)
     lse = _lse(LSE, Q, device)
-    n = _ints(counts, "counts", (batch.view.B,), device)
+    n = None if counts is None else _ints(counts, "counts", (batch.view.B,), device)
     if workspace is None:
         workspace = _workspace_on(stream, device, cqsa_cache_weigh_workspace, cache, batch, Q)
     space, size = _place(workspace, device)
@@ -829,11 +843,11 @@ def cqsa_cache_evict(cache, batch, W, new_lengths, budget, first=0, recent=0, to
 def _probs(t, name, device):
     """The bytes of t's cqsa_probs."""
     s, n = t.stride(), t.shape
-    code = _dtypes().get(t.dtype)
+    code = (_dtype_table or _dtypes()).get(t.dtype)
     if code is None or t.device != device or len(s) != 3 or (n[2] > 1 and s[2] != 1):
         raise ValueError(f"{name} must be a float32, float16 or bfloat16 tensor [B, rows, V] on {device} with "
                          "contiguous rows")
-    return _PROBS.pack(t.data_ptr(), code, n[0], n[1], n[2], s[0], s[1])
+    return _PROBS.pack(t.data_ptr(), code, *n, s[0], s[1])
 
 
 def cqsa_draft_verify_workspace(target, draft=None):

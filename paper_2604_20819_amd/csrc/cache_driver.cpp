@@ -202,27 +202,27 @@ Range cache_range(const cqsa_cache* c) {
 // Shape, alignment and strides of numbers for B sequences' tokens; `written`: they must not overlap.
 cqsa_status check_weights(const cqsa_weights* w, const char* name, const cqsa_cache* c, const cqsa_cache_batch* b,
                           int64_t tokens, bool written, const std::string& what) {
-  const std::string n = what + name;
-  if (!w) return fail(CQSA_ERR_INVALID_ARG, n + " is NULL");
+  auto bad = [&](const std::string& text) { return fail(CQSA_ERR_INVALID_ARG, what + name + text); };
+  if (!w) return bad(" is NULL");
   if (w->B != b->B || w->H != c->H)
-    return fail(CQSA_ERR_INVALID_ARG, n + "'s B and H differ from the batch's and the cache's");
+    return bad("'s B and H differ from the batch's and the cache's");
   if (w->T < tokens || w->T > (int64_t(1) << 31))
-    return fail(CQSA_ERR_INVALID_ARG, n + " must have T = " + std::to_string(tokens) + " or more, below 2^31");
+    return bad(" must have T = " + std::to_string(tokens) + " or more, below 2^31");
   if (w->B == 0 || w->T == 0) return CQSA_OK;
   if (!w->data || reinterpret_cast<uintptr_t>(w->data) % 4 != 0)
-    return fail(CQSA_ERR_INVALID_ARG, n + ".data is NULL or not 4-byte aligned");
+    return bad(".data is NULL or not 4-byte aligned");
   struct Axis {
     int64_t n, stride;
   } ax[2] = {{w->B, w->stride_b}, {w->H, w->stride_h}};
   for (const Axis& a : ax)
     if (a.n > 1 && (a.stride < 0 || a.stride > (int64_t(1) << 40)))
-      return fail(CQSA_ERR_INVALID_ARG, n + "'s strides must be in [0, 2^40]");
+      return bad("'s strides must be in [0, 2^40]");
   if (!written) return CQSA_OK;
   if (ax[0].stride < ax[1].stride) std::swap(ax[0], ax[1]);
   int64_t span = w->T;  // of the tokens, then with the axis of the smaller stride too
   for (int i = 1; i >= 0; --i) {
     if (ax[i].n == 1) continue;
-    if (ax[i].stride < span) return fail(CQSA_ERR_INVALID_ARG, n + " is written and overlaps itself");
+    if (ax[i].stride < span) return bad(" is written and overlaps itself");
     span += ax[i].stride * (ax[i].n - 1);
   }
   return CQSA_OK;
