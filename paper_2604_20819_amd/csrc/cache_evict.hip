@@ -77,8 +77,21 @@ __device__ __forceinline__ bool shares(uint32_t k, uint32_t border, int pass) {
   return pass == 0 || (pass == 1 ? k >> 21 == border >> 21 : k >> 10 == border >> 10);
 }
 
+// Inclusive sums over the lanes.
+__device__ __forceinline__ int scan_of_wave(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // within rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // rows 0 and 2 into 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // the lower half into the upper
+  return x;
+}
+
 // The digit in which the `left`-th largest of the counted keys lies: counts of kBins in
-// `count` (LDS or memory), by the NT threads of a work group.  `scratch`: a word a wave and 2.
+// `count` (LDS or memory), by the NT threads of a work group.  `scratch`: a word a wave and 3.
+// Where all keys that share the digits so far are kept the border is below them, and left is 0:
+// no digit has to follow.
 template <int NT>
 __device__ __forceinline__ EvictBorder next_digit(const uint32_t* count, const EvictBorder& at, int pass, int* scratch) {
   constexpr int PER = kBins / NT, WAVES = NT / 64;
@@ -86,12 +99,7 @@ __device__ __forceinline__ EvictBorder next_digit(const uint32_t* count, const E
   int mine[PER], sum = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) sum += mine[i] = int(count[kBins - 1 - (tid * PER + i)]);  // from the largest down
-  int run = sum;
-#pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const int y = __shfl_up(run, k);
-    if (lane >= k) run += y;
-  }
+  const int run = scan_of_wave(sum);
   if (lane == 63) scratch[wave] = run;
   __syncthreads();
   int above = run - sum;
@@ -102,14 +110,15 @@ __device__ __forceinline__ EvictBorder next_digit(const uint32_t* count, const E
       if (above < at.left && above + mine[i] >= at.left) {
         scratch[WAVES] = kBins - 1 - (tid * PER + i);
         scratch[WAVES + 1] = at.left - above;
+        scratch[WAVES + 2] = mine[i];
       }
       above += mine[i];
     }
   }
   __syncthreads();
   const uint32_t d = uint32_t(scratch[WAVES]);
-  const EvictBorder next = {at.key | (pass == 0 ? d << 21 : pass == 1 ? d << 10 : d), scratch[WAVES + 1]};
-  __syncthreads();
+  EvictBorder next = {at.key | (pass == 0 ? d << 21 : pass == 1 ? d << 10 : d), scratch[WAVES + 1]};
+  if (next.left == scratch[WAVES + 2]) next = {next.key ? next.key - 1 : 0u, 0};
   return next;
 }
 
@@ -146,7 +155,7 @@ struct Counts {
   }
 };
 
-constexpr EvictBorder kNothing = {kForced, 0};  // of a sequence that keeps nothing
+constexpr EvictBorder kNothing = {kForced, 0};  // of a sequence that keeps nothing, of 0 tokens
 
 __device__ __forceinline__ int kept_of(const EvictArgs& a, int present) { return present < a.budget ? present : a.budget; }
 
@@ -158,7 +167,7 @@ template <int ITEMS>
 __global__ void __launch_bounds__(1024, 8) cache_evict_select(const EvictArgs a) {
   constexpr int WAVES = 16, NT = 64 * WAVES;
   __shared__ uint32_t count[kBins];
-  __shared__ int scratch[WAVES + 2];
+  __shared__ int scratch[WAVES + 3];
   __shared__ int before[2][WAVES];
   const int64_t id = (int64_t(blockIdx.y) << kGridLog2) + blockIdx.x;
   const int h = int(id % a.c.H), b = int(id / a.c.H);
@@ -203,8 +212,8 @@ __global__ void __launch_bounds__(1024, 8) cache_evict_select(const EvictArgs a)
     at = kNothing;
   } else {
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-      if (pass > 0) {
+    for (int pass = 0; pass < 3 && at.left > 0; ++pass) {
+      if (pass > 0) {  // (a barrier lies behind the last reads of the counts and of scratch)
         for (int i = tid; i < kBins; i += NT) count[i] = 0;
         __syncthreads();
       }
@@ -257,14 +266,11 @@ __device__ __forceinline__ EvictBorder border_of(const EvictArgs& a, int64_t id,
   EvictBorder at;
   if (PASS == 1) {
     at = {0u, kept_of(a, len - int(words[3 * kBins]))};
+    if (at.left == 0) at = kNothing;
   } else {
     at = a.state[id * 3 + PASS - 2];
   }
-  if (at.left == 0) {
-    at = kNothing;
-  } else {
-    at = next_digit<256>(words + (PASS - 1) * kBins, at, PASS - 1, scratch);
-  }
+  if (at.left > 0) at = next_digit<256>(words + (PASS - 1) * kBins, at, PASS - 1, scratch);
   if (leave && threadIdx.x == 0) a.state[id * 3 + PASS - 1] = at;
   return at;
 }
@@ -272,7 +278,7 @@ __device__ __forceinline__ EvictBorder border_of(const EvictArgs& a, int64_t id,
 template <int PASS>
 __global__ void __launch_bounds__(256) cache_evict_count(const EvictArgs a, int per) {
   __shared__ uint32_t count[kBins];
-  __shared__ int scratch[6];
+  __shared__ int scratch[7];
   const int64_t id = blockIdx.x / per;
   const int part = blockIdx.x % per;
   const int h = int(id % a.c.H), b = int(id / a.c.H);
@@ -280,6 +286,7 @@ __global__ void __launch_bounds__(256) cache_evict_count(const EvictArgs a, int 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = length_of(a.c, b);
   const EvictBorder at = border_of<PASS>(a, id, len, part == 0, scratch);
+  if ((PASS == 1 || PASS == 2) && at.left == 0) return;  // known by now
   const float* w = a.w.p + b * a.w.b + h * a.w.h;
   uint32_t* words = a.counts + id * kHeadWords;
   if (PASS < 3) {
