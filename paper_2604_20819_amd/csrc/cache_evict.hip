@@ -5,7 +5,7 @@
 // weight's bits in an order that integers compare by, and 2^32 - 1 for the first and
 // the recent tokens.  The n-th largest key is found by its digits of 11, 11 and 10
 // bits, from counts of the keys that share its upper ones: integers, whose sums go in
-// any order.  A head's tokens up to 16384 are a work group's, which holds their keys in
+// any order.  A head's tokens up to 32768 are a work group's, which holds their keys in
 // registers; longer ones are shared by many, with the counts in memory.
 #include <algorithm>
 
@@ -162,9 +162,10 @@ __device__ __forceinline__ int kept_of(const EvictArgs& a, int present) { return
 }  // namespace
 
 // A work group takes all of a head's tokens, 16 waves of 64 ITEMS in a row, whose keys stay in registers.
-// What bounds it is issuing the 100 instructions or so that 64 keys cost in all.
+// What bounds it is issuing the 100 instructions or so that 64 keys cost in all, and a chain of loads and
+// barriers where they are few (8 heads of 1000 tokens 8.3 us, of 16384 14.7; 512 heads of 16384 29).
 template <int ITEMS>
-__global__ void __launch_bounds__(1024, 8) cache_evict_select(const EvictArgs a) {
+__global__ void __launch_bounds__(1024, ITEMS > 16 ? 4 : 8) cache_evict_select(const EvictArgs a) {
   constexpr int WAVES = 16, NT = 64 * WAVES;
   __shared__ uint32_t count[kBins];
   __shared__ int scratch[WAVES + 3];
@@ -461,7 +462,9 @@ __global__ void __launch_bounds__(256) cache_evict_move(const EvictArgs a, int t
 // ------------------------------------------------------------------ launching
 EvictPlan plan_evict(int64_t B, int64_t H, int64_t max_len) {
   EvictPlan p{};
-  if (max_len <= 16 * 1024) return p;
+  // 8 heads of 32768 tokens: 23 us by a work group each, 32 by shared ones (of 65536 50 and 32);
+  // 512 heads 59 and 104 (149 and 169)
+  if (max_len <= 32 * 1024) return p;
   p.chunks = int((max_len + kChunk - 1) / kChunk);
   p.counts = B * H * kHeadWords;
   return p;
@@ -472,8 +475,10 @@ hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t s) {
   if (a.chunks == 0) {
     if (a.c.max_len <= 4096)
       hipLaunchKernelGGL((cache_evict_select<4>), attend_grid(heads), dim3(1024), 0, s, a);
-    else
+    else if (a.c.max_len <= 16384)
       hipLaunchKernelGGL((cache_evict_select<16>), attend_grid(heads), dim3(1024), 0, s, a);
+    else
+      hipLaunchKernelGGL((cache_evict_select<32>), attend_grid(heads), dim3(1024), 0, s, a);
   } else {
     const int64_t words = heads * kHeadWords;
     const int per = int(std::min<int64_t>(a.chunks, std::max<int64_t>(1, (int64_t(1) << 22) / heads)));
