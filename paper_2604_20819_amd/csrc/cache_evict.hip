@@ -380,7 +380,9 @@ __global__ void __launch_bounds__(256) cache_evict_place(const EvictArgs a, int 
 // A wave moves 32 kept tokens of a head.  STAGED: from the stage into the pages, in their
 // places; else from the pages into the stage (in place) or the target's pages.  A lane's four
 // source tokens are the same for all channel pairs, whose 4 bytes it gathers one by one:
-// the cache holds values by channel pairs, so that any token moved touches all of its tile.
+// the cache holds values by channel pairs, so that any token moved touches all of its tile.  The
+// bytes bound it (64 sequences of up to 16384 tokens down to 4096, 8 heads, d = 128: 617 MB read and
+// 260 written in 187 us, 4.7 TB/s; by work groups of 4 waves for 32 tokens, with barriers, 316).
 template <bool STAGED>
 __global__ void __launch_bounds__(256) cache_evict_move(const EvictArgs a, int tiles) {
   const CacheArgs& c = a.c;

@@ -48,7 +48,11 @@ constexpr int weigh_few_waves(int parts, int db, int nq) {
 }  // namespace
 
 // Few rows, 16 NQ at most: they stay in registers while a wave goes through the
-// tokens in tiles of 32, the next tile's keys on their way.
+// tokens in tiles of 32, the next tile's keys on their way.  The keys' bytes and the
+// weights bound it where they are many (one token of 2^20, 8 heads, d = 128: 637 MB in 126
+// us, 5.1 TB/s; a copy reaches 4.9), a chain of loads, 4.4 us, where they are few.  Two
+// tiles at a time, for more loads on their way, were 3 % slower for long sequences and as much
+// faster for short ones, and spilled from d = 224 on.
 template <typename T, int DB, int NQ>
 __global__ void __launch_bounds__(256, (weigh_few_waves(RowType<T>::kQuery, DB, NQ))) cache_weigh_few(const WeighArgs a, int per_seq) {
   constexpr bool WIDE = DB % 4 == 0;  // whole blocks a lane
@@ -199,6 +203,11 @@ __global__ void __launch_bounds__(256, (weigh_few_waves(RowType<T>::kQuery, DB, 
 // where a matrix operand lies as the 64 lanes read it.  RESIDENT: all rows fit the two
 // stages that LDS holds; they are brought once, and the work group goes on to every
 // `tiles`-th of its sequence's 64 W tokens, the next ones' keys on their way.
+// Exponentials bound it, beside the products: 3 vector instructions a weight, one of them
+// of 16 cycles, and d / 16 products of 32 cycles for 32 x 32 weights (4096 rows of 4 heads over
+// 32768 tokens, d = 128: 478 us, 1090 TFLOP/s, vector units 62 % busy, matrix cores 48 %; d = 64:
+// 363).  Products issued among the exponentials of the 32 rows before were as fast at d = 128
+// (529 us both, with 8 waves) and 30 % slower at d = 64, whose registers then leave half the waves.
 template <typename T, int DB, int W, int RS, bool RESIDENT>
 __global__ void __launch_bounds__(64 * W, W > 8 ? 4 : sizeof(T) == 4 && W == 4 && DB > 6 ? 1 : 2)
     cache_weigh_many(const WeighArgs a, int tiles, int splits) {

@@ -4,7 +4,8 @@
 // is replaced by one drawn from max(0, p - q), which leaves the target's
 // distribution.  Of the K + 1 rows of probabilities that a sequence has only the
 // one at its first refusal (or behind its last draft) is read, once: that bounds
-// it where sequences are many, and some 8 us of dependent loads where they are few.
+// it where sequences are many (256 of 100003 tokens in fp32: 102 MB in 21 us, 4.9 TB/s),
+// and two kernels of 4 us, chains of loads, where they are few (one of 32000 tokens 8 us).
 //
 // The draw inverts the sum over the vocabulary: a wave sums each of up to 256 pieces, and
 // the piece in which the sum passes the drawn share is gone through again.
