@@ -560,8 +560,8 @@ typedef struct {
  *   W[b][h][t] = decay prior[b][h][t] + sum over i of exp(s_it - LSE_i),   0 <= t < lengths[b].
  * Q, LSE (fp32 [B, H_q, L]), causal and scale as in cqsa_cache_attend, which leaves that LSE.  prior (or
  * NULL: zeros) is read at the tokens that were there before the call's rows, t < lengths[b] - n_b; the rows'
- * own tokens start from 0 whatever it holds, and with decay = 0 all do.  prior may be W itself, else it lies apart from it (which is
- * checked).  W from lengths[b] on is left as it was.  counts: int32 [B] in device memory, or NULL: the sums
+ * own tokens start from 0 whatever it holds, and with decay = 0 all do.  prior may be W itself, else it lies apart from it; so do
+ * the other arguments, Q from its first element to its last (all of which is checked).  W from lengths[b] on is left as it was.  counts: int32 [B] in device memory, or NULL: the sums
  * go over the first counts[b] rows of sequence b alone (taken into [0, n_b]), as where the other rows'
  * drafts were rejected.  Rows whose LSE is not finite (they saw nothing, or a NaN) add nothing; tokens whose
  * page holds nothing get nothing.  decay: in [0, 1].  Scores and sums are fp32 for every dtype; the order of
@@ -596,7 +596,7 @@ typedef struct {
  * The batch's q_start and max_q are not read.  W: T at least max_len; W_to: T at least the smaller of budget
  * and max_len, apart from W (checked).  to's tables have pages for that many tokens (checked).
  * kept (or NULL): int32 [B, H, budget], the positions that the kept tokens had, -1 behind them.
- * new_lengths: int32 [B], may be batch.lengths.
+ * new_lengths: int32 [B], may be batch.lengths; else what is written lies apart from the other arguments (checked).
  * B H is at most 2^23, and at most 2^27 tiles of 32 tokens may be kept.  workspace as in
  * cqsa_cache_attend, by cqsa_cache_evict_workspace. */
 cqsa_status cqsa_cache_evict(const cqsa_cache* cache, const cqsa_cache_batch* batch,

@@ -251,6 +251,11 @@ cqsa_status check_weigh(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   return CQSA_OK;
 }
 
+Range tables_range(const char* name, const cqsa_cache_batch* b) {
+  if (!b || b->B == 0) return {name, 0, 0};
+  return range_of(name, b->pages, 4 * (uint64_t(b->B - 1) * uint64_t(b->pages_stride) + uint64_t(b->max_pages)));
+}
+
 cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view* Q, const float* LSE,
                        const int32_t* counts, const cqsa_weights* prior, float decay, const cqsa_weights* W,
                        int32_t causal, float scale, void* workspace, uint64_t workspace_bytes, hipStream_t s) {
@@ -274,10 +279,12 @@ cqsa_status weigh_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqs
   if ((st = check_workspace(workspace, workspace_bytes, need, what)) != CQSA_OK) return st;
   const Range w = weights_range("W", W);
   const bool in_place = prior && same_weights(*prior, *W);
-  if ((st = check_apart({w, range_of("the workspace", workspace, need)}, {range_of("LSE", LSE, uint64_t(Q->B) * Q->L * Q->H * 4), cache_range(c),
-                              in_place ? Range{"", 0, 0} : weights_range("prior", prior),
-                              range_of("counts", counts, 4 * uint64_t(b->B)),
-                              range_of("the lengths", b->lengths, 4 * uint64_t(b->B))},
+  const uint64_t four = 4 * uint64_t(b->B);
+  if ((st = check_apart({w, range_of("the workspace", workspace, need)},
+                        {range_of("LSE", LSE, uint64_t(Q->B) * Q->L * Q->H * 4), cache_range(c),
+                         in_place ? Range{"", 0, 0} : weights_range("prior", prior), range_of("counts", counts, four),
+                         range_of("the lengths", b->lengths, four), tables_range("the pages", b),
+                         range_of("q_start", b->q_start, four + 4), view_range("Q", *Q)},
                         what)) != CQSA_OK)
     return st;
   WeighArgs a{};
@@ -371,7 +378,8 @@ cqsa_status evict_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cqs
   if ((st = check_apart({range_of("kept", kept, 4 * heads * uint64_t(o->budget)),
                          range_of("new_lengths", new_lengths, four), cache_range(c),
                          range_of("the workspace", workspace, e.bytes), weights_range("W_to", W_to), to ? none : w},
-                        {to ? w : none, new_lengths == b->lengths ? none : range_of("the lengths", b->lengths, four)},
+                        {to ? w : none, new_lengths == b->lengths ? none : range_of("the lengths", b->lengths, four),
+                         tables_range("the pages", b), tables_range("to's pages", to)},
                         what)) != CQSA_OK)
     return st;
   cqsa_view rows{};  // the call has none

@@ -55,6 +55,10 @@ __int128 extent(const cqsa_view& v) {
 }
 }  // namespace
 
+Range view_range(const char* name, const cqsa_view& v) {
+  return range_of(name, v.data, empty(v) ? 0 : uint64_t(extent(v) * elem_bytes(v.dtype)));
+}
+
 bool same_place(const cqsa_view& x, const cqsa_view& y) {
   auto same = [](int64_t n, int64_t a, int64_t b) { return n == 1 || a == b; };
   return x.data == y.data && same(x.B, x.stride_b, y.stride_b) && same(x.L, x.stride_l, y.stride_l) &&

@@ -32,6 +32,8 @@ inline Range range_of(const char* name, const void* p, uint64_t bytes) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(p);
   return {name, at, p ? at + bytes : at};
 }
+// From a view's first element to its last.
+Range view_range(const char* name, const cqsa_view& v);
 inline cqsa_status check_workspace(const void* p, uint64_t bytes, uint64_t need, const std::string& what) {
   if (need == 0) return CQSA_OK;
   if (!p || bytes < need)

@@ -67,6 +67,10 @@ def test_weigh_refused():
     refused(weigh(counts=PTR + FAR), "W overlaps counts")
     refused(weigh(counts=PTR + 1), "4-byte")
     refused(weigh(w=weights(data=PTR)), "W overlaps the cache")
+    refused(weigh(b=batch(pages=PTR + FAR + 8)), "W overlaps the pages")
+    refused(weigh(b=batch(lengths=PTR + FAR + 9592)), "W overlaps the lengths")
+    refused(weigh(q=view(H=8, data=PTR + FAR - 64)), "W overlaps Q")
+    refused(weigh(q=view(B=1, L=6, H=8, data=PTR + 3 * FAR), b=batch(q_start=PTR + FAR, max_q=6)), "W overlaps q_start")
     refused(weigh(b=batch(lengths=None)), "lengths is NULL")
     refused(weigh(b=batch(pages=None)), "pages is NULL")
     assert cq.lib().cqsa_cache_weigh(cache(), batch(), view(H=8), PTR, None, None, 1.0, None, 1, 0.0, None, 0, None) == -1
@@ -139,6 +143,8 @@ def test_evict_refused():
     refused(evict(kept=PTR + FAR + 1200), "kept overlaps W")
     refused(evict(kept=PTR + 2 * FAR), "kept overlaps new_lengths")
     refused(evict(b=batch(lengths=PTR + 2 * FAR - 4)), "new_lengths overlaps the lengths")
+    refused(evict(kept=PTR + 6 * FAR), "kept overlaps the pages")
+    refused(evict(to=tables(), new=PTR + 3 * FAR + 36), "new_lengths overlaps to's pages")
     refused(evict(space=None), "workspace")
     refused(evict(space=SPACE + 8), "workspace")
     refused(evict(space=PTR), "overlaps the workspace")

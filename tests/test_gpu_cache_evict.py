@@ -238,6 +238,65 @@ def test_more_sequences_and_heads_than_one_dimension_takes():
     assert torch.equal(W_to, torch.where(gone, 7.0, W.gather(-1, want.clamp(max=31))))
 
 
+def test_weights_far_apart():
+    """Weights and pages whose bytes lie past 2^31."""
+    need_gpu()
+    say("evict far")
+    H, d, page = 2, 256, 256
+    per = cq.cqsa_cache_page_bytes(page, H, d)
+    m = 2 ** 31 // per + 40
+    cache = cq.Cache4(m, H, d, page_size=page)
+    pages = torch.tensor([[m - 1, m - 3], [m - 5, 1]], dtype=torch.int32, device="cuda")
+    to = torch.tensor([[0], [m - 7]], dtype=torch.int32, device="cuda")
+    g = torch.Generator("cuda").manual_seed(1)
+    for i in pages.flatten().tolist():
+        cache.data[i] = torch.randint(0, 256, (per,), generator=g, device="cuda", dtype=torch.uint8)
+        cache.data[i].view(-1, 34 * d)[:, 32 * d:] = 120
+    lengths = torch.tensor([500, 300], dtype=torch.int32, device="cuda")
+    batch = cq.CacheBatch(pages, lengths)
+    far = 2 ** 31 + 777
+    store = torch.empty(far + 10 ** 5, device="cuda")
+    W = store.as_strided((2, H, 512), (far, 600, 1))
+    W.copy_(torch.rand(2, H, 512, generator=g, device="cuda"))
+    new = torch.zeros(2, dtype=torch.int32, device="cuda")
+    kept = torch.zeros(2, H, 200, dtype=torch.int32, device="cuda")
+    cq.cqsa_cache_evict(cache, batch, W, new, 200, to=to, kept=kept)
+    assert new.tolist() == [200, 200]
+    k, v = torch.empty(2, 2, 500, H, d, device="cuda").unbind(0)
+    cq.cqsa_cache_read(cache, batch, k, v)
+    k2, v2 = torch.empty(2, 2, 200, H, d, device="cuda").unbind(0)
+    cq.cqsa_cache_read(cache, cq.CacheBatch(to, new), k2, v2)
+    for b, n in enumerate((500, 300)):
+        for h in range(H):
+            best = W[b, h, :n].topk(200).indices.sort().values
+            assert torch.equal(kept[b, h].long(), best)
+            assert torch.equal(k2[b, :, h], k[b, 500 - n + best, h]) and torch.equal(v2[b, :, h], v[b, 500 - n + best, h])
+
+
+def test_python_refusals():
+    need_gpu()
+    case = case_of(12, [40, 30], 2, 64, 32, 10)
+    cache, batch = case.cache(), case.batch()
+    W, n = torch.rand(2, 2, 96, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    to = torch.from_numpy(case.target).cuda()
+    kept = torch.zeros(2, 2, 10, dtype=torch.int32, device="cuda")
+    ok = dict(cache=cache, batch=batch, W=W, new_lengths=n, budget=10)
+    for bad in (dict(W=W.cpu()), dict(W=W.double()), dict(new_lengths=n.long()), dict(new_lengths=n[:1]), dict(budget=-1),
+                dict(budget=2 ** 31), dict(first=-1), dict(to=to.long()), dict(to=to[:1]), dict(to=to.cpu()), dict(kept=kept[..., :9]),
+                dict(kept=kept.float()), dict(to=to, W_to=W[0]), dict(workspace=torch.zeros(10 ** 6, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            cq.cqsa_cache_evict(**{**ok, **bad})
+    for bad in (dict(budget=0), dict(first=6, recent=5), dict(W=W[..., :50]), dict(W_to=W), dict(to=to, W_to=W), dict(new_lengths=None),
+                dict(workspace=torch.zeros(16, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(cq.CqsaError):
+            cq.cqsa_cache_evict(**{**ok, **bad})
+    before = cache.data.clone()
+    cq.cqsa_cache_evict(**ok, to=to)
+    rest = torch.ones(case.n_pages, dtype=torch.bool, device="cuda")
+    rest[to[to >= 0].long()] = False
+    assert torch.equal(cache.data[rest], before[rest]) and n.tolist() == [10, 10]
+
+
 def test_strided_weights_another_stream_and_capture():
     need_gpu()
     say("evict captured")

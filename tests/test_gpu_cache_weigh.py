@@ -288,6 +288,46 @@ def test_strided_tensors_and_another_stream():
     assert (store == 7).all()
 
 
+def test_weights_far_apart():
+    """Weights whose elements lie past 2^31."""
+    need_gpu()
+    say("weigh far")
+    case = Case(13, [90, 70], 2, 64, 32)
+    case.fill_tokens()
+    cache, batch = case.cache(), case.batch()
+    T, far = case.table.shape[1] * 32, 2 ** 31 + 12345
+    for L in (2, 100):
+        q = normal(case.g, (2, L, 2, 64), "bf16").cuda()
+        lse = attended(case, cache, batch, q, True)
+        store = torch.empty(far + 10 ** 6, device="cuda")
+        W = store.as_strided((2, 2, T), (far, T + 3, 1))
+        W.fill_(7.0)
+        cq.cqsa_cache_weigh(cache, batch, q, lse, W)
+        check(case, q, lse, W, [L, L], None, True, 0.125, None, 1.0, False)
+        cq.cqsa_cache_weigh(cache, batch, q, lse, W, prior=W, decay=0.5)
+        assert torch.isfinite(W).all()
+
+
+def test_python_refusals():
+    need_gpu()
+    case = Case(14, [40, 30], 2, 64, 32)
+    cache, batch = case.cache(), case.batch()
+    q = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    lse, W = torch.zeros(2, 4, 3, device="cuda"), torch.zeros(2, 2, 96, device="cuda")
+    n = torch.zeros(2, dtype=torch.int32, device="cuda")
+    ok = dict(cache=cache, batch=batch, Q=q, LSE=lse, W=W)
+    for bad in (dict(Q=q.cpu()), dict(Q=q[0]), dict(LSE=lse[:, :2]), dict(LSE=lse.double()), dict(W=W.half()), dict(W=W[0]),
+                dict(W=W.transpose(1, 2)), dict(prior=W.cpu()), dict(counts=n[:1]), dict(counts=n.long()),
+                dict(workspace=torch.zeros(8, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            cq.cqsa_cache_weigh(**{**ok, **bad})
+    for bad in (dict(W=W[..., :50]), dict(W=W[:1].expand(2, -1, -1)), dict(prior=W[..., 1:].as_strided((2, 2, 96), (96, 96, 1))),
+                dict(decay=2.0), dict(scale=math.inf)):
+        with pytest.raises(cq.CqsaError):
+            cq.cqsa_cache_weigh(**{**ok, **bad})
+    cq.cqsa_cache_weigh(**ok)
+
+
 def test_same_bits_again_and_captured():
     """Two calls give the same bits, and so does every replay of a captured one."""
     need_gpu()

@@ -154,6 +154,50 @@ def test_numbers_that_are_none_and_tokens_outside():
     assert (out == -1).all() and (n_out == 1).all()
 
 
+def test_subnormal_probabilities():
+    need_gpu()
+    say("verify subnormal")
+    p, q, tokens, u = inputs(7, 3, 2, 400, "f32")
+    for f in (1e-38, 1e-41):
+        a, b = (p.double() * f).float(), (q.double() * f).float()
+        run(a, b, tokens, u)
+        run(a, None, tokens, u)
+
+
+def test_rows_far_apart():
+    """Rows whose elements lie past 2^31."""
+    need_gpu()
+    say("verify far")
+    V, far = 1001, 2 ** 31 + 10 ** 6
+    p, q, tokens, u = inputs(8, 2, 1, V, "bf16")
+    store = torch.empty(far + 3 * 10 ** 6, dtype=torch.bfloat16, device="cuda")
+    P = store.as_strided((2, 2, V), (far, 10 ** 5 + 1, 1))
+    Q = store.as_strided((2, 1, V), (far, V, 1), 10 ** 6 + 7)
+    P.copy_(p)
+    Q.copy_(q)
+    run(P, Q, tokens, u)
+    P = store.as_strided((2, 2, V), (10 ** 6, far, 1))
+    P.copy_(p)
+    run(P, None, tokens, u)
+
+
+def test_python_refusals():
+    need_gpu()
+    p, q, tokens, u = (x.cuda() for x in inputs(9, 2, 2, 64, "f32"))
+    out, n = torch.zeros(2, 3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    ok = dict(target=p, draft=q, tokens=tokens, u=u, out=out, n_out=n)
+    for bad in (dict(target=p.cpu()), dict(target=p.double()), dict(target=p[0]), dict(draft=q.transpose(1, 2)), dict(draft=q.cpu()),
+                dict(tokens=tokens.long()), dict(tokens=tokens[:1]), dict(u=u.double()), dict(u=u[:, :2]), dict(out=out[:, :2]),
+                dict(n_out=n.cpu()), dict(counts=n.float()), dict(workspace=torch.zeros(64, dtype=torch.uint8)),
+                dict(lengths=n, new_lengths=n.long())):
+        with pytest.raises(ValueError):
+            cq.cqsa_draft_verify(**{**ok, **bad})
+    for bad in (dict(lengths=n), dict(draft=q.half()), dict(draft=p), dict(out=tokens.new_zeros(2, 3), n_out=None)):
+        with pytest.raises(cq.CqsaError):
+            cq.cqsa_draft_verify(**{**ok, **bad})
+    cq.cqsa_draft_verify(**ok)
+
+
 def test_odd_strides_and_alignment():
     """Rows that begin at any element, broadcast targets, rows that lie apart."""
     need_gpu()
