@@ -214,6 +214,68 @@ def test_long_sequences(n, budget, kind):
         assert torch.equal(y[0].transpose(0, 1), want)
 
 
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("n,budget", [(4000, 900), (5000, 4999), (16000, 3000), (20000, 150), (40000, 12000), (90000, 30011)])
+def test_long_batches_with_holes_and_strange_weights(n, budget, in_place):
+    """Every way of choosing: ties, NaN, infinities, pages that hold nothing, a sequence with none and one without tokens."""
+    need_gpu()
+    say("evict long batch", n, budget, in_place)
+    H, d, page, first, recent = 2, 32, 128, 5, 100
+    lens = [n, n // 3, 700, 0]
+    need = [-(-x // page) for x in lens]
+    g = torch.Generator("cuda").manual_seed(n)
+    pool = sum(need) * 2 + 1
+    order = torch.randperm(pool, generator=g, device="cuda").int()
+    pages = torch.full((4, need[0] + 1), -1, dtype=torch.int32, device="cuda")
+    to = pages.clone()
+    for b, m in enumerate(need):
+        pages[b, :m] = order[sum(need[:b]):sum(need[:b]) + m]
+        to[b, :m] = order[sum(need) + sum(need[:b]):sum(need) + sum(need[:b]) + m]
+    if not in_place:
+        pages[0, [0, 3, need[0] - 1]] = -1
+        pages[1, 2] = pool
+        pages[2] = -5
+    data = torch.randint(0, 256, (pool, cq.cqsa_cache_page_bytes(page, H, d)), generator=g, device="cuda", dtype=torch.uint8)
+    data.view(pool, -1, 34 * d)[..., 32 * d:] = 124
+    cache = cq.Cache4(pool, H, d, page_size=page, data=data)
+    lengths = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    batch = cq.CacheBatch(pages, lengths, max_len=n)
+    W = torch.randn(4, H, n + 3, generator=g, device="cuda")
+    odd = torch.tensor([0.0, -0.0, math.nan, math.inf, -math.inf, 1e-42, 1.0, -1.0], device="cuda")
+    pick = torch.randint(0, 40, W.shape, generator=g, device="cuda")
+    W = torch.where(pick < 8, odd[pick.clamp(max=7)], W)
+    k, v = torch.zeros(2, 4, n, H, d, device="cuda").unbind(0)
+    cq.cqsa_cache_read(cache, batch, k, v)
+    t = torch.arange(n, device="cuda")
+    rank = torch.where(torch.isnan(W), -1e302, W.double().clamp(-1e301, 1e301))[..., :n]
+    L = lengths[:, None]
+    forced = (t < first) | (t >= L - recent)
+    entry = pages[:, t // page]
+    there = (t < L) & (entry >= 0) & (entry < pool)
+    rank = rank.masked_fill(forced[:, None], 1e303).masked_fill(~there[:, None], -1e303)
+    keep = there.sum(-1).clamp(max=budget)
+    best = torch.sort(rank, dim=-1, descending=True, stable=True).indices[..., :budget]
+    gone = (torch.arange(best.shape[-1], device="cuda") >= keep[:, None])[:, None]
+    best = best.masked_fill(gone, n).sort(-1).values
+    old, new = W.clone(), torch.zeros(4, dtype=torch.int32, device="cuda")
+    kept = torch.full((4, H, budget), 9, dtype=torch.int32, device="cuda")
+    W_to = None if in_place else torch.full((4, H, n), 7.0, device="cuda")
+    cq.cqsa_cache_evict(cache, batch, W, new, budget, first, recent, to=None if in_place else to, W_to=W_to, kept=kept)
+    assert torch.equal(new.long(), keep)
+    assert torch.equal(kept.long(), torch.where(best < n, best, -1))
+    after = cq.CacheBatch(pages if in_place else to, new, max_len=n)
+    k2, v2 = torch.zeros(2, 4, budget, H, d, device="cuda").unbind(0)
+    cq.cqsa_cache_read(cache, after, k2, v2)
+    got = (W if in_place else W_to).view(torch.int32)
+    for b in range(4):
+        m = int(keep[b])
+        for h in range(H):
+            src = best[b, h, :m]
+            assert torch.equal(got[b, h, :m], old[b, h].view(torch.int32)[src])
+            row = n - lens[b] + src  # what was read ends with the sequence's last token
+            assert torch.equal(k2[b, budget - m:, h], k[b, row, h]) and torch.equal(v2[b, budget - m:, h], v[b, row, h])
+
+
 def test_more_sequences_and_heads_than_one_dimension_takes():
     need_gpu()
     say("evict many heads")
