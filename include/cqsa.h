@@ -567,7 +567,7 @@ typedef struct {
  * page holds nothing get nothing.  decay: in [0, 1].  Scores and sums are fp32 for every dtype; the order of
  * a sum goes by the sizes of the call's arguments alone.
  * T of W and prior is at least batch.max_len.  workspace as in cqsa_cache_attend, by
- * cqsa_cache_weigh_workspace; the limits on a launch are that call's too. */
+ * cqsa_cache_weigh_workspace.  That call's limits hold, and B H ceil(max_len / 256) is at most 2^27. */
 cqsa_status cqsa_cache_weigh(const cqsa_cache* cache, const cqsa_cache_batch* batch,
                              const cqsa_view* Q, const float* LSE, const int32_t* counts,
                              const cqsa_weights* prior, float decay, const cqsa_weights* W,
