@@ -164,6 +164,8 @@ __device__ __forceinline__ int kept_of(const EvictArgs& a, int present) { return
 // A work group takes all of a head's tokens, 16 waves of 64 ITEMS in a row, whose keys stay in registers.
 // What bounds it is issuing the 100 instructions or so that 64 keys cost in all, and a chain of loads and
 // barriers where they are few (8 heads of 1000 tokens 8.3 us, of 16384 14.7; 512 heads of 16384 29).
+// The fewer keys a lane holds the shorter that chain: 8 heads of 2111 tokens 6.4 us with 4, with 16
+// 10.3; 512 heads of 4096 10.5 and 13.6.
 template <int ITEMS>
 __global__ void __launch_bounds__(1024, ITEMS > 16 ? 4 : 8) cache_evict_select(const EvictArgs a) {
   constexpr int WAVES = 16, NT = 64 * WAVES;

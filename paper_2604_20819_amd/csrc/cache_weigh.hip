@@ -36,8 +36,12 @@ __device__ __forceinline__ RowShift row_shift(const WeighArgs& a, const Seq& s, 
 }
 constexpr RowShift kBlindRow = {INFINITY, 0};
 
-// Groups of 16 rows that the kernel for few rows takes in registers.
-constexpr int weigh_few_groups(int parts, int db) { return parts * db <= 8 ? 2 : 1; }
+// Groups of 16 rows that the kernel for few rows takes in registers.  A second one pays at d = 128
+// and 256, with 8 operands a group at most (64 sequences of up to 8192 tokens, 8 heads, 24 and 32
+// rows: bf16 d = 128 49 and 53 us, from LDS 56 and 52; fp16 d = 128 63 and 67, 80 and 75; bf16
+// d = 256 107 and 110, 113 and 108), not elsewhere (bf16 d = 64 43 and 47, from LDS 39 and 36;
+// d = 96 64 and 65, 50 and 46; d = 160 91 and 95, 78 and 74; fp32 d = 64 57 and 63, 53 and 50).
+constexpr int weigh_few_groups(int parts, int db) { return db % 4 == 0 && parts * db <= 8 ? 2 : 1; }
 // Waves a SIMD is to hold: as many as the registers allow without spilling.
 constexpr int weigh_few_waves(int parts, int db, int nq) {
   const int held = parts * db * nq;
@@ -209,7 +213,7 @@ __global__ void __launch_bounds__(256, (weigh_few_waves(RowType<T>::kQuery, DB, 
 // 363).  Products issued among the exponentials of the 32 rows before were as fast at d = 128
 // (529 us both, with 8 waves) and 30 % slower at d = 64, whose registers then leave half the waves.
 template <typename T, int DB, int W, int RS, bool RESIDENT>
-__global__ void __launch_bounds__(64 * W, W > 8 ? 4 : sizeof(T) == 4 && W == 4 && DB > 6 ? 1 : 2)
+__global__ void __launch_bounds__(64 * W, W > 8 ? 4 : 2)
     cache_weigh_many(const WeighArgs a, int tiles, int splits) {
   constexpr int D = 32 * DB, QP = RowType<T>::kQuery, NT = 64 * W, TOKENS = 64 * W;
   constexpr int UNITS = RS * 4 * DB, NU = (UNITS + NT - 1) / NT;  // of 8 elements
@@ -470,17 +474,22 @@ constexpr int stage_rows(int parts, int db) { return parts * db <= 8 ? 64 : 32; 
 // (4 sequences of 2000, d = 128, 89; with 16 129).
 constexpr int kShortWaves = 4;
 constexpr int long_waves(int db) { return db <= 4 ? 16 : 8; }
+// And over resident rows: 4, or 8 where their stages leave LDS for one work group a CU (fp32 d = 256,
+// 64 sequences of up to 8192 tokens: 32 rows 161 us, 217 with 4 waves, 64 rows 238 and 332; over 4
+// sequences of 1000 16 and 13; d = 192 191 and 177).
+constexpr int resident_waves(int parts, int db) { return parts * db > 18 ? 8 : 4; }
 
 template <typename T, int DB>
 void launch_d(const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
-  constexpr int QP = RowType<T>::kQuery, NQ = weigh_few_groups(QP, DB), RS = stage_rows(QP, DB), LW = long_waves(DB);
+  constexpr int QP = RowType<T>::kQuery, NQ = weigh_few_groups(QP, DB), RS = stage_rows(QP, DB), LW = long_waves(DB),
+                RW = resident_waves(QP, DB);
   const dim3 grid = attend_grid(p.groups), block(64 * p.waves);
   if (p.row_groups == 0) {
     if (p.resident)
-      hipLaunchKernelGGL((cache_weigh_many<T, DB, kShortWaves, RS, true>), grid, block, 0, s, a, p.tiles, 1);
+      hipLaunchKernelGGL((cache_weigh_many<T, DB, RW, RS, true>), grid, block, 0, s, a, p.tiles, 1);
     else if (p.waves == LW)
       hipLaunchKernelGGL((cache_weigh_many<T, DB, LW, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
-    else
+    else if constexpr (DB <= 4 || QP < 3)
       hipLaunchKernelGGL((cache_weigh_many<T, DB, kShortWaves, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
   } else if (p.row_groups == 1) {
     hipLaunchKernelGGL((cache_weigh_few<T, DB, 1>), grid, block, 0, s, a, p.tiles);
@@ -538,24 +547,31 @@ WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t tokens, int64_t
     return p;
   }
   if (rows <= 2 * stage) {
-    // the same with tiles of 256 tokens, 4 a work group (48 rows, 64 sequences of up to 8192
+    // the same with tiles of 64 tokens a wave, 4 a work group (48 rows, 64 sequences of up to 8192
     // tokens, d = 128: 67 us, one 100; 128 rows, 16 of them 37 and 48)
     p.resident = true;
-    const int64_t most = (max_len + 255) / 256;
-    p.tiles = int(std::max<int64_t>(1, std::min(most, std::max<int64_t>(1536 / heads, B == 1 ? 0 : most / 4))));
+    p.waves = resident_waves(parts, db);
+    const int64_t most = (max_len + 64 * p.waves - 1) / (64 * p.waves), fit = 6144 / p.waves / heads;
+    p.tiles = int(std::max<int64_t>(1, std::min(most, std::max<int64_t>(fit, B == 1 ? 0 : most / 4))));
     p.groups = heads * p.tiles;
     return p;
   }
-  // Long: most tokens were there before the rows, so that the waves of a work group all have rows.
-  const bool far = max_len >= 8192 && max_len >= 2 * tokens;
-  if (db <= 4 ? far : max_len > 1536 && dt != CQSA_F32) p.waves = long_waves(db);
+  // More waves where most tokens were there before the rows, so that all waves of a work group have
+  // rows (bf16, 32 heads over 8, d = 128: 1024 rows over 16384 tokens 149 us, with 4 waves 178; 4096
+  // over 8192 263 and 257); up to d = 64 a single sequence only, since those of a batch have lengths
+  // of their own (d = 64: 4096 over 32768 745 and 825, 2048 over 8192 115 and 110; 8 of up to 16384
+  // tokens, 1024 rows, 545 and 472).  Past d = 128 wherever there are enough tokens for the larger
+  // work groups (d = 256, 8 sequences of 2000 225 and 288), in fp32 always (32 of 300 128 and 242,
+  // 8 of 2000 518 and 997; d = 192 112 and 131, 410 and 789, 1024 rows over 1500 tokens 62 and 55).
+  const bool far = max_len >= 4 * tokens && (db > 2 ? max_len >= 8192 : B == 1 && max_len * db >= 32768);
+  if (db <= 4 ? far : max_len > 1536 || dt == CQSA_F32) p.waves = long_waves(db);
   p.tiles = int((max_len + 64 * p.waves - 1) / (64 * p.waves));
   // The rows are split until the GPU has 8 work groups of 4 waves a CU, which evens out what causal
   // masks leave of them (32 sequences of 300 tokens and rows of 4 heads, d = 128: 31 us in 3 or 4 parts,
   // 54 in one; 4 of 2000 89 in 8, 159 in 2), or as many as their registers allow (d = 256: 32 of 300
-  // 56 in 2, 61 in 3; fp32, 2 of 1000 94 in 8, 118 in 24), or 2 of more waves; of 128 rows at least.
+  // 56 in 2, 61 in 3), or 2 of more waves; of 128 rows at least.
   const int64_t groups = heads * p.tiles;
-  const int64_t total = p.waves > 4 || (db > 4 && dt == CQSA_F32) ? 512 : db > 4 ? 1024 : 2048;
+  const int64_t total = p.waves > 4 ? 512 : db > 4 ? 1024 : 2048;
   const int64_t most = std::min<int64_t>(rows / 128, 64);
   p.splits = int(std::max<int64_t>(1, std::min(most, (total + groups - 1) / groups)));
   p.groups = groups * p.splits;
