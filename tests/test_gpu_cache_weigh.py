@@ -119,6 +119,29 @@ def test_long_contexts(d, n, L, page, dtype):
     run(case, 4, [L] * 3, dtype, counts=[L, L - 7, L], decay=0.5, oracle=ob.weigh_rows if n > 1000 else ob.weigh)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d,n,L", [(32, 32771, 35), (64, 16390, 40), (64, 16384, 33)])
+def test_one_long_context(d, n, L, dtype):
+    """A single sequence, for whose narrow heads work groups have more waves only then."""
+    need_gpu()
+    say("weigh one long", d, n, L, dtype)
+    case = Case(n + d, [n], 1, d, 128)
+    any_tokens(case)
+    case.table[0, 1] = -1
+    run(case, 4, [L], dtype, decay=0.5, oracle=ob.weigh_rows)
+
+
+@pytest.mark.parametrize("d", [192, 224, 256])
+@pytest.mark.parametrize("n,G", [(33, 1), (16, 4), (11, 4), (13, 5)])
+def test_rows_held_for_wide_heads(d, n, G):
+    """33 to 65 fp32 rows over more tokens than a work group's, and fewer."""
+    need_gpu()
+    say("weigh wide", d, n, G)
+    case = Case(d + n, [1100, 515, 40, 5], 2, d, 64)
+    any_tokens(case)
+    run(case, 2 * G, [n] * 4, "f32", decay=0.75)
+
+
 @pytest.mark.parametrize("rows", [1, 2, 4, 5, 16, 17, 32, 33, 63, 64, 65, 127, 128, 129, 192, 257])
 def test_row_counts(rows):
     """Around the borders between the kernels, and a kernel's own steps."""
