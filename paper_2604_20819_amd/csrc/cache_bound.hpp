@@ -34,8 +34,8 @@ struct WeighPlan {
   int splits;      // and over its rows
   int64_t groups;  // work groups in all
 };
-// rows: the most that a sequence and key head has, of `tokens` tokens.
-WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t tokens, int64_t max_len, cqsa_dtype dt, int d);
+// rows: the most that a sequence and key head has.
+WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d);
 
 // The key at which a head's kept tokens end.
 struct EvictBorder {

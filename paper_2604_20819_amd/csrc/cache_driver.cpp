@@ -237,7 +237,7 @@ TokenWeights weights_of(const cqsa_weights* w) {
 // The launch of a call whose arguments check_attend has passed, and its workspace.
 WeighPlan weigh_plan(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view& Q) {
   const int64_t n = empty(Q) ? 0 : b->q_start ? b->max_q : Q.L;
-  return plan_weigh(b->B, c->H, n * (Q.H / c->H), n, b->max_len, Q.dtype, c->d);
+  return plan_weigh(b->B, c->H, n * (Q.H / c->H), b->max_len, Q.dtype, c->d);
 }
 uint64_t weigh_bytes(const WeighPlan& p, const cqsa_cache* c, const cqsa_cache_batch* b) {
   return p.splits == 1 ? 0 : uint64_t(p.splits) * uint64_t(b->B) * uint64_t(c->H) * uint64_t(b->max_len) * 4;

@@ -467,13 +467,25 @@ namespace {
 
 // Rows of a stage, so that two of them fit LDS.
 constexpr int stage_rows(int parts, int db) { return parts * db <= 8 ? 64 : 32; }
-// Waves of a work group over long contexts, which go through more rows a byte of LDS the more
-// they are, as many as the registers of their keys allow (4096 rows of 4 heads over 32768 tokens,
-// bf16: d = 128 478 us, with 8 waves 560, with 4 554; d = 64 355, 350 and 358; d = 256, 2048
-// rows, 449 with 8, 564 with 4), and over short ones, which more work groups share more evenly
-// (4 sequences of 2000, d = 128, 89; with 16 129).
+// Waves of a work group: 4, or more, which go through more rows a byte of LDS, as many as the
+// registers of their keys allow.
 constexpr int kShortWaves = 4;
 constexpr int long_waves(int db) { return db <= 4 ? 16 : 8; }
+// More wherever 4 have no second work group's registers beside them (fp32 past d = 128: 8 sequences of
+// 2000 tokens, 4 heads a group, d = 256 338 us, 997 before).  Else where work groups have much of the same
+// length: not over many sequences, whose lengths differ, and not over few tokens (1 of 8192 tokens and rows,
+// bf16 d = 128 307 us, with 4 waves 333; 4096 rows over 32768 508 and 601; of 3000 72 and 67; 64 of up to 4000,
+// 200 rows, 16 heads a group, 387 and 312; fp16 d = 128, 4 of up to 3000, 198 and 230; d = 160, 64 of 200
+// over 4000, 638 and 599).  4 waves spill at bf16 d = 256 (64 of 200 over 4000 530, with 4 606; of 700 180
+// and 157).  Narrow heads, whose rows take little LDS, have no use for more (bf16 d = 64: 1 of 8192 236, with
+// 4 215; d = 32 206 and 169).
+constexpr bool has_long(int parts, int db) { return db > 4 || (db > 1 && parts * db > 2); }
+constexpr bool has_short(int parts, int db) { return db <= 4 || parts < 3; }
+bool takes_long(int parts, int db, int64_t B, int64_t max_len) {
+  if (!has_long(parts, db) || !has_short(parts, db)) return has_long(parts, db);
+  if (db > 4) return max_len > 1536 && (B <= 4 / parts || parts * db == 8);
+  return parts * db == 8 ? B <= 8 && max_len >= 2048 : B <= 4 && max_len >= 8192;
+}
 // And over resident rows: 4, or 8 where their stages leave LDS for one work group a CU (fp32 d = 256,
 // 64 sequences of up to 8192 tokens: 32 rows 161 us, 217 with 4 waves, 64 rows 238 and 332; over 4
 // sequences of 1000 16 and 13; d = 192 191 and 177).
@@ -487,10 +499,12 @@ void launch_d(const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
   if (p.row_groups == 0) {
     if (p.resident)
       hipLaunchKernelGGL((cache_weigh_many<T, DB, RW, RS, true>), grid, block, 0, s, a, p.tiles, 1);
-    else if (p.waves == LW)
-      hipLaunchKernelGGL((cache_weigh_many<T, DB, LW, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
-    else if constexpr (DB <= 4 || QP < 3)
-      hipLaunchKernelGGL((cache_weigh_many<T, DB, kShortWaves, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
+    if constexpr (has_long(QP, DB))
+      if (!p.resident && p.waves == LW)
+        hipLaunchKernelGGL((cache_weigh_many<T, DB, LW, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
+    if constexpr (has_short(QP, DB))
+      if (!p.resident && p.waves == kShortWaves)
+        hipLaunchKernelGGL((cache_weigh_many<T, DB, kShortWaves, RS, false>), grid, block, 0, s, a, p.tiles, p.splits);
   } else if (p.row_groups == 1) {
     hipLaunchKernelGGL((cache_weigh_few<T, DB, 1>), grid, block, 0, s, a, p.tiles);
   } else if constexpr (NQ == 2) {
@@ -525,7 +539,7 @@ hipError_t launch_rows(const WeighArgs& a, const WeighPlan& p, hipStream_t s) {
 
 }  // namespace
 
-WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t tokens, int64_t max_len, cqsa_dtype dt, int d) {
+WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_dtype dt, int d) {
   WeighPlan p{};
   const int parts = dt == CQSA_F32 ? 3 : (dt == CQSA_F16 ? 2 : 1), db = d / 32, stage = stage_rows(parts, db);
   const int64_t heads = B * H;
@@ -556,24 +570,20 @@ WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t tokens, int64_t
     p.groups = heads * p.tiles;
     return p;
   }
-  // More waves where most tokens were there before the rows, so that all waves of a work group have
-  // rows (bf16, 32 heads over 8, d = 128: 1024 rows over 16384 tokens 149 us, with 4 waves 178; 4096
-  // over 8192 263 and 257); up to d = 64 a single sequence only, since those of a batch have lengths
-  // of their own (d = 64: 4096 over 32768 745 and 825, 2048 over 8192 115 and 110; 8 of up to 16384
-  // tokens, 1024 rows, 545 and 472).  Past d = 128 wherever there are enough tokens for the larger
-  // work groups (d = 256, 8 sequences of 2000 225 and 288), in fp32 always (32 of 300 128 and 242,
-  // 8 of 2000 518 and 997; d = 192 112 and 131, 410 and 789, 1024 rows over 1500 tokens 62 and 55).
-  const bool far = max_len >= 4 * tokens && (db > 2 ? max_len >= 8192 : B == 1 && max_len * db >= 32768);
-  if (db <= 4 ? far : max_len > 1536 || dt == CQSA_F32) p.waves = long_waves(db);
+  if (takes_long(parts, db, B, max_len)) p.waves = long_waves(db);
   p.tiles = int((max_len + 64 * p.waves - 1) / (64 * p.waves));
   // The rows are split until the GPU has 8 work groups of 4 waves a CU, which evens out what causal
   // masks leave of them (32 sequences of 300 tokens and rows of 4 heads, d = 128: 31 us in 3 or 4 parts,
-  // 54 in one; 4 of 2000 89 in 8, 159 in 2), or as many as their registers allow (d = 256: 32 of 300
-  // 56 in 2, 61 in 3), or 2 of more waves; of 128 rows at least.
+  // 54 in one), or as many as their registers allow (d = 256: 32 of 300 56 in 2, 61 in 3), or 2 of more
+  // waves; of 128 rows at least.  And into parts of 512 rows up to 8, of 1024 from there on, where the lengths
+  // of sequences differ (64 of up to 746 tokens and rows, 16 heads a group, d = 160: 222 us, without 445; fp32
+  // 676 and 1281; 64 of up to 700, 4 heads, fp32 d = 256 350, in parts of 1024 529), of 2048 for one alone
+  // (of 8192 307, of 1024 319), up to 2^14 work groups, which bounds the workspace by max_len.
   const int64_t groups = heads * p.tiles;
   const int64_t total = p.waves > 4 ? 512 : db > 4 ? 1024 : 2048;
+  const int64_t even = B == 1 ? rows / 2048 : std::max<int64_t>(rows / 1024, std::min<int64_t>(rows / 512, 8));
   const int64_t most = std::min<int64_t>(rows / 128, 64);
-  p.splits = int(std::max<int64_t>(1, std::min(most, (total + groups - 1) / groups)));
+  p.splits = int(std::max<int64_t>(1, std::min(most, std::max((total + groups - 1) / groups, std::min(even, 16384 / groups)))));
   p.groups = groups * p.splits;
   return p;
 }
