@@ -577,11 +577,13 @@ WeighPlan plan_weigh(int64_t B, int64_t H, int64_t rows, int64_t max_len, cqsa_d
   // 54 in one), or as many as their registers allow (d = 256: 32 of 300 56 in 2, 61 in 3), or 2 of more
   // waves; of 128 rows at least.  And into parts of 512 rows up to 8, of 1024 from there on, where the lengths
   // of sequences differ (64 of up to 746 tokens and rows, 16 heads a group, d = 160: 222 us, without 445; fp32
-  // 676 and 1281; 64 of up to 700, 4 heads, fp32 d = 256 350, in parts of 1024 529), of 2048 for one alone
-  // (of 8192 307, of 1024 319), up to 2^14 work groups, which bounds the workspace by max_len.
+  // 676 and 1281; 64 of up to 700, 4 heads, fp32 d = 256 350, in parts of 1024 529), up to 2^14 work
+  // groups, which bounds the workspace by max_len.  One alone is split into parts of 2048 rows by 4 waves (4096
+  // rows of 4 heads over 32768, bf16 d = 64: 361 us, of 4096 393) and no further by more (d = 128 483 and 502).
   const int64_t groups = heads * p.tiles;
   const int64_t total = p.waves > 4 ? 512 : db > 4 ? 1024 : 2048;
-  const int64_t even = B == 1 ? rows / 2048 : std::max<int64_t>(rows / 1024, std::min<int64_t>(rows / 512, 8));
+  const int64_t even = B == 1 ? (p.waves > 4 ? 0 : rows / 2048)
+                              : std::max<int64_t>(rows / 1024, std::min<int64_t>(rows / 512, 8));
   const int64_t most = std::min<int64_t>(rows / 128, 64);
   p.splits = int(std::max<int64_t>(1, std::min(most, std::max((total + groups - 1) / groups, std::min(even, 16384 / groups)))));
   p.groups = groups * p.splits;
