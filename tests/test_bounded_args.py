@@ -99,6 +99,19 @@ def test_weigh_workspace():
         assert n.value < 1 << 30
 
 
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("d", [32, 128, 256])
+def test_weigh_workspace_of_long_bounds(d, dtype):
+    """The parts of a split call are bounded, however long a bound the caller gives for the lengths."""
+    n = ctypes.c_uint64()
+    for B, L, Hq, max_len in ((1, 65536, 64, 1 << 24), (7, 4096, 64, 1 << 20), (1000, 4096, 64, 1 << 20), (64, 4096, 128, 4096),
+                              (2, 8192, 32, 8192)):
+        c, q = cache(d=d, n_pages=1 << 20), view(B=B, L=L, H=Hq, d=d, dtype=dtype)
+        b = batch(B=B, max_len=max_len, max_pages=max_len, pages_stride=max_len)
+        assert cq.lib().cqsa_cache_weigh_workspace(c, b, q, n) == 0, cq.lib().cqsa_last_error()
+        assert n.value <= 1 << 27
+
+
 # -------------------------------------------------------------------- evict
 def opts(budget=100, first=0, recent=0):
     return cq.cqsa_evict_opts(budget, first, recent)
