@@ -245,6 +245,8 @@ uint64_t weigh_bytes(const WeighPlan& p, const cqsa_cache* c, const cqsa_cache_b
 cqsa_status check_weigh(const cqsa_cache* c, const cqsa_cache_batch* b, const cqsa_view* Q, const std::string& what) {
   const cqsa_status st = check_attend(c, b, Q, what);
   if (st != CQSA_OK) return st;
+  // check_rows looks at max_q only where there are rows; without them the tokens' prior is still read
+  if (b->q_start && b->max_q < 0) return fail(CQSA_ERR_INVALID_ARG, what + "max_q must be 0 or more");
   const int64_t heads = int64_t(b->B) * c->H, tiles = (int64_t(b->max_len) + 255) / 256;
   if (heads > (int64_t(1) << 23) || heads * tiles > kMaxGroups)
     return fail(CQSA_ERR_UNSUPPORTED, what + "more sequences, heads and tokens than one launch takes");

@@ -82,6 +82,18 @@ def test_weigh_refused():
     assert weigh(b=batch(max_len=0, lengths=None), w=weights(T=0, data=None)) == 0
 
 
+def test_weigh_without_rows_and_a_negative_bound_refused():
+    """n_b would be max_q, below 0, and prior be read behind its tokens."""
+    n = ctypes.c_uint64()
+    none = view(B=1, L=0, H=8, data=None)
+    b = batch(q_start=PTR + 5 * FAR, max_q=-5, lengths=None)  # no lengths: the call ends at its checks in any case
+    refused(weigh(b=b, q=none, prior=weights()), "max_q")
+    refused(cq.lib().cqsa_cache_weigh_workspace(cache(), b, none, n), "max_q")
+    b.max_q = 0
+    refused(weigh(b=b, q=none, prior=weights()), "lengths is NULL")
+    assert cq.lib().cqsa_cache_weigh_workspace(cache(), b, none, n) == 0 and n.value == 0
+
+
 def test_weigh_workspace():
     n = ctypes.c_uint64(7)
     assert cq.lib().cqsa_cache_weigh_workspace(cache(), batch(), view(H=8), n) == 0
