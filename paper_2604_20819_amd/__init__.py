@@ -733,7 +733,7 @@ def _place(workspace, device):
 def _lse(LSE, Q, device):
     """The address of an LSE for the rows of Q."""
     B, L, H, _ = Q.shape
-    if LSE.dtype is not _torch().float32 or LSE.device != device or not LSE.is_contiguous() or LSE.shape != (B, H, L):
+    if LSE is None or LSE.dtype is not _torch().float32 or LSE.device != device or not LSE.is_contiguous() or LSE.shape != (B, H, L):
         raise ValueError(f"LSE must be a contiguous float32 tensor of shape (B, H, L) = {(B, H, L)} on {device}")
     return LSE.data_ptr()
 
@@ -755,8 +755,8 @@ def cqsa_cache_attend(cache, batch, Q, O, LSE=None, causal=True, scale=0.0, work
 # ------------------------------- cached tokens' weights, eviction, drafted tokens
 def _weights(t, name, device):
     """The bytes of t's cqsa_weights."""
-    s, n = t.stride(), t.shape
-    if t.dtype is not _torch().float32 or t.device != device or len(s) != 3 or (s[2] != 1 and n[2] > 1):
+    s, n = (t.stride(), t.shape) if t is not None else ((), ())
+    if len(s) != 3 or t.dtype is not _torch().float32 or t.device != device or (s[2] != 1 and n[2] > 1):
         raise ValueError(f"{name} must be a float32 tensor [B, H, T] on {device} with contiguous tokens")
     return _WEIGHTS.pack(t.data_ptr(), *n, s[0], s[1])
 
@@ -842,9 +842,9 @@ def cqsa_cache_evict(cache, batch, W, new_lengths, budget, first=0, recent=0, to
 
 def _probs(t, name, device):
     """The bytes of t's cqsa_probs."""
-    s, n = t.stride(), t.shape
-    code = (_dtype_table or _dtypes()).get(t.dtype)
-    if code is None or t.device != device or len(s) != 3 or (n[2] > 1 and s[2] != 1):
+    s, n = (t.stride(), t.shape) if t is not None else ((), ())
+    code = (_dtype_table or _dtypes()).get(t.dtype) if len(s) == 3 else None
+    if code is None or t.device != device or (n[2] > 1 and s[2] != 1):
         raise ValueError(f"{name} must be a float32, float16 or bfloat16 tensor [B, rows, V] on {device} with "
                          "contiguous rows")
     return _PROBS.pack(t.data_ptr(), code, *n, s[0], s[1])
@@ -865,13 +865,13 @@ def cqsa_draft_verify(target, draft, tokens, u, out, n_out, counts=None, lengths
     the draft's [B, K, V] (None: tokens that come without), by random numbers u (fp32 [B, K + 1] in
     [0, 1)), and draw the token behind the accepted ones.  out (int32 [B, K + 1]) gets them, -1 behind, n_out
     (int32 [B]) how many; new_lengths those of the cache without the refused ones' rows."""
-    device = target.device
-    if not target.is_cuda:
+    if target is None or not target.is_cuda:
         raise ValueError("target must live on a GPU")
+    device = target.device
     p = _probs(target, "target", device)
     q = None if draft is None else _probs(draft, "draft", device)
     B, K = target.shape[0], target.shape[1] - 1
-    if u.dtype != _torch().float32 or u.device != device or not u.is_contiguous() or u.shape != (B, K + 1):
+    if u is None or u.dtype != _torch().float32 or u.device != device or not u.is_contiguous() or u.shape != (B, K + 1):
         raise ValueError(f"u must be a contiguous float32 tensor of shape {(B, K + 1)} on {device}")
     one, few = (B,), (B, K + 1)
     tokens, counts = _ints(tokens, "tokens", (B, K), device), _ints(counts, "counts", one, device)

@@ -124,6 +124,18 @@ def test_weigh_workspace_of_long_bounds(d, dtype):
         assert n.value <= 1 << 27
 
 
+def test_missing_tensors_are_named():
+    """The binding's checks of tensors that a call cannot do without; None is refused as other wrong ones are."""
+    import torch
+    q = torch.zeros(2, 3, 4, 64)
+    with pytest.raises(ValueError, match="LSE must be"):
+        cq._lse(None, q, q.device)
+    with pytest.raises(ValueError, match="W must be"):
+        cq._weights(None, "W", q.device)
+    with pytest.raises(ValueError, match="target must be"):
+        cq._probs(None, "target", q.device)
+
+
 # -------------------------------------------------------------------- evict
 def opts(budget=100, first=0, recent=0):
     return cq.cqsa_evict_opts(budget, first, recent)

@@ -351,6 +351,20 @@ def test_python_refusals():
     cq.cqsa_cache_weigh(**ok)
 
 
+def test_missing_arguments_are_named():
+    need_gpu()
+    case = Case(14, [40, 30], 2, 64, 32)
+    cache, batch = case.cache(), case.batch()
+    q = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    lse, W = torch.zeros(2, 4, 3, device="cuda"), torch.zeros(2, 2, 96, device="cuda")
+    with pytest.raises(ValueError, match="LSE must"):
+        cq.cqsa_cache_weigh(cache, batch, q, None, W)
+    with pytest.raises(ValueError, match="W must"):
+        cq.cqsa_cache_weigh(cache, batch, q, lse, None)
+    with pytest.raises(ValueError, match="W must"):
+        cq.cqsa_cache_evict(cache, batch, None, torch.zeros(2, dtype=torch.int32, device="cuda"), 10)
+
+
 def test_same_bits_again_and_captured():
     """Two calls give the same bits, and so does every replay of a captured one."""
     need_gpu()

@@ -198,6 +198,19 @@ def test_python_refusals():
     cq.cqsa_draft_verify(**ok)
 
 
+def test_missing_arguments_are_named():
+    need_gpu()
+    p, q, tokens, u = (x.cuda() for x in inputs(9, 2, 2, 64, "f32"))
+    out, n = torch.zeros(2, 3, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    ok = dict(target=p, draft=q, tokens=tokens, u=u, out=out, n_out=n)
+    for name in ("target", "u"):
+        with pytest.raises(ValueError, match=name + " must"):
+            cq.cqsa_draft_verify(**{**ok, name: None})
+    for name in ("tokens", "out", "n_out"):
+        with pytest.raises(cq.CqsaError, match=name + " is NULL"):
+            cq.cqsa_draft_verify(**{**ok, name: None})
+
+
 def test_odd_strides_and_alignment():
     """Rows that begin at any element, broadcast targets, rows that lie apart."""
     need_gpu()
