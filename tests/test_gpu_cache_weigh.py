@@ -290,6 +290,52 @@ def test_sums_are_the_rows():
         assert torch.allclose(W.double().sum(-1), torch.full((B, 2), 2.0 * L, dtype=torch.float64, device="cuda"), rtol=1e-4)
 
 
+@pytest.mark.parametrize("d,dtype,G,max_len", [(32, "bf16", 8, 2 ** 20), (64, "f16", 1, 2 ** 20), (64, "f32", 8, 2 ** 20),
+                                               (128, "bf16", 8, 2 ** 19), (160, "f32", 8, 2 ** 19)])
+def test_sums_of_many_rows(d, dtype, G, max_len):
+    """Weights of 131072 rows that are all alike: the roundings of one long sum, in which equal terms are
+    added, would all go the same way (2e-5 of the sum and more).
+
+    Half steps of a sum: 2 LSE for the exponent (LSE in powers of two, rounded twice), 2 for the exponential,
+    4 and 32 for the rows that a lane adds before it compensates what it loses, 2 for that sum itself, 2 for
+    the lanes' and W's."""
+    need_gpu()
+    say("weigh many rows", d, dtype, G, max_len)
+    H, rows, n, page = 8, 131072, 300, 256
+    pages = torch.full((1, max_len // page), -1, dtype=torch.int32, device="cuda")
+    pages[0, :2] = torch.tensor([1, 0])
+    cache = cq.Cache4(2, H, d, page_size=page)  # zeros: every score is 0
+    # the bound on the lengths gives work groups enough that the rows are not split
+    batch = cq.CacheBatch(pages, torch.tensor([n], dtype=torch.int32, device="cuda"), max_len=max_len)
+    q = torch.zeros(1, rows // G, H * G, d, dtype=DT[dtype], device="cuda")
+    assert cq.cqsa_cache_weigh_workspace(cache, batch, q) is None
+    lse = (1.1 + 0.37 * torch.arange(H, device="cuda")).repeat_interleave(G)[None, :, None].expand(1, H * G, rows // G).contiguous()
+    W = torch.full((1, H, max_len), 7.0, device="cuda")
+    cq.cqsa_cache_weigh(cache, batch, q, lse, W, causal=False)
+    e = lse[0, ::G, 0].double()
+    want = (rows * torch.exp(-e))[:, None]
+    off = ((W[0, :, :n].double() - want) / want).abs()
+    assert (off <= ((2 * e + 44) * HALF)[:, None]).all(), off.max().item()
+    assert (W[0, :, n:] == 7).all()
+
+
+def test_sums_past_the_last_number():
+    """Weights that are infinite, by an LSE that no attention left, give an infinite sum, not a NaN."""
+    need_gpu()
+    say("weigh infinite sums")
+    H, d, rows, max_len = 2, 32, 4096, 2 ** 16
+    pages = torch.full((1, max_len // 256), -1, dtype=torch.int32, device="cuda")
+    pages[0, 0] = 0
+    cache = cq.Cache4(1, H, d, page_size=256)
+    batch = cq.CacheBatch(pages, torch.tensor([90], dtype=torch.int32, device="cuda"), max_len=max_len)
+    q = torch.zeros(1, rows, H, d, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(1, H, rows, device="cuda")
+    lse[0, 1, 100] = -100.0
+    W = torch.zeros(1, H, max_len, device="cuda")
+    cq.cqsa_cache_weigh(cache, batch, q, lse, W, causal=False)
+    assert (W[0, 0, :90] == rows).all() and (W[0, 1, :90] == math.inf).all()
+
+
 def test_strided_tensors_and_another_stream():
     need_gpu()
     say("weigh strides")
