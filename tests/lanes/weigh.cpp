@@ -1,7 +1,7 @@
 // One call of the attention weights' kernels on the CPU, in buffers of exact sizes, twice in other orders of
 // its waves and work groups, against a sum in 64 bits.
 //   weigh name=value ... lens=a,b,... [new=a,b,...]
-// Prints the launch.  Ends with 1 where a weight is off by more than its roundings, or goes by the order.
+// Prints the launch, and with dry=1 no more than that.  Ends with 1 where a weight is off by more than its roundings, or goes by the order.
 #include "cache_weigh.hip"
 
 #include <stdio.h>
@@ -52,6 +52,17 @@ int main(int argc, char** argv) {
   std::mt19937 g(arg("seed", 1));
   auto real = [&]() { return float(int(g() % 2001) - 1000) / 1000; };
 
+  WeighPlan p = plan_weigh(B, H, int64_t(L) * G, max_len, dt, d);
+  if (const int tiles = arg("tiles", 0)) {  // fewer work groups over the tokens, so that each goes through several tiles
+    if (p.row_groups == 0 && !p.resident) return 2;
+    p.tiles = tiles, p.groups = int64_t(B) * H * tiles;
+  }
+  const int each = p.row_groups ? 32 : 64;  // tokens of a wave's tile
+  printf("row_groups %d resident %d waves %d tiles %d splits %d a_wave %d\n", p.row_groups, p.resident, p.waves, p.tiles, p.splits,
+         (max_len + each * p.waves * p.tiles - 1) / (each * p.waves * p.tiles));
+  fflush(stdout);
+  if (arg("dry", 0)) return 0;
+
   const int columns = std::max(1, (max_len + P - 1) / P);
   int64_t n_pages = 1, rows = packed ? 0 : L;
   for (int n : lens) n_pages += (n + P - 1) / P;
@@ -93,17 +104,8 @@ int main(int argc, char** argv) {
   if (prior) a.prior = in_place ? a.w : TokenWeights{before.p, int64_t(H) * max_len, max_len};
   a.Hq = Hq, a.G = G, a.causal = causal, a.decay = decay;
   a.scale_log2 = scale * 1.4426950408889634f;
-  WeighPlan p = plan_weigh(B, H, int64_t(L) * G, max_len, dt, d);
-  if (const int tiles = arg("tiles", 0)) {  // fewer work groups over the tokens, so that each goes through several tiles
-    if (p.row_groups == 0 && !p.resident) return 2;
-    p.tiles = tiles, p.groups = heads * tiles;
-  }
   Buffer<float> part(p.splits > 1 ? p.splits * heads * max_len : 0);
   a.part = p.splits > 1 ? part.p : nullptr;
-  const int each = p.row_groups ? 32 : 64;  // tokens of a wave's tile
-  printf("row_groups %d resident %d waves %d tiles %d splits %d a_wave %d\n", p.row_groups, p.resident, p.waves, p.tiles, p.splits,
-         (max_len + each * p.waves * p.tiles - 1) / (each * p.waves * p.tiles));
-  fflush(stdout);
 
   std::vector<float> first;
   for (int run = 0; run < 2; ++run) {

@@ -60,3 +60,12 @@ class Case:
 
 def starts(new, first=0):
     return torch.tensor(np.concatenate([[first], first + np.cumsum(new)]).astype(np.int32)).cuda()
+
+
+# Calls of cqsa_cache_weigh whose waves go through several tiles of tokens, one after the other: sequences, heads,
+# query heads a head, rows, d, dtype, the longest sequence.
+WEIGH_LOOPS = [
+    (16, 16, 1, 1, 32, "bf16", 4100), (3, 64, 8, 2, 128, "f16", 3001), (2, 64, 5, 6, 128, "bf16", 5000),
+    (2, 96, 3, 4, 96, "f32", 2777), (1, 256, 1, 1, 32, "bf16", 50003),  # few rows; more than 64 tiles
+    (8, 64, 5, 9, 64, "bf16", 3000), (5, 96, 1, 100, 96, "f16", 2100), (4, 64, 4, 12, 256, "f32", 3100),  # rows that stay
+]

@@ -15,7 +15,7 @@ import paper_2604_20819_amd as cq
 from oracle import bounded as ob
 from oracle import cache4 as o4
 from tests.gpu_util import need_gpu, say
-from tests.op_util import DT, Case, normal, starts
+from tests.op_util import DT, WEIGH_LOOPS, Case, normal, starts
 
 pytestmark = pytest.mark.gpu
 HALF = 2.0 ** -24
@@ -334,6 +334,54 @@ def test_sums_past_the_last_number():
     W = torch.zeros(1, H, max_len, device="cuda")
     cq.cqsa_cache_weigh(cache, batch, q, lse, W, causal=False)
     assert (W[0, 0, :90] == rows).all() and (W[0, 1, :90] == math.inf).all()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,H,G,L,d,dtype,n", WEIGH_LOOPS)
+def test_waves_of_several_tiles(B, H, G, L, d, dtype, n, in_place):
+    """Keys, pages and prior of a wave's next tile are read while it works on one: every token's own prior, and
+    a page that holds nothing among them.  (tests/test_operator_lanes.py: that these calls' waves go through several.)"""
+    need_gpu()
+    say("weigh loops", B, H, G, L, d, dtype, n, in_place)
+    page, scale = 64, 1 / math.sqrt(d)
+    lens = [n if b == 0 else int(n * (b * 0.6180339887 % 1.0)) for b in range(B)]
+    g = torch.Generator("cuda").manual_seed(n + d)
+    need = [-(-x // page) for x in lens]
+    pages = torch.full((B, need[0]), -1, dtype=torch.int32, device="cuda")
+    order = torch.randperm(sum(need), generator=g, device="cuda").int()
+    for b, m in enumerate(need):
+        pages[b, :m] = order[sum(need[:b]):sum(need[:b]) + m]
+    pages[0, need[0] // 2] = -1
+    data = torch.randint(0, 256, (sum(need), cq.cqsa_cache_page_bytes(page, H, d)), generator=g, device="cuda", dtype=torch.uint8)
+    data.view(sum(need), -1, 34 * d)[..., 32 * d:] = 121 + data.view(sum(need), -1, 34 * d)[..., 32 * d:] % 3
+    cache = cq.Cache4(sum(need), H, d, page_size=page, data=data)
+    lengths = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    batch = cq.CacheBatch(pages, lengths, max_len=n)
+    q = torch.randn(B, L, H * G, d, generator=g, device="cuda").to(DT[dtype])
+    lse = attended(None, cache, batch, q, True)
+    prior = torch.rand(B, H, n, generator=g, device="cuda") + 0.5
+    before = prior.double()
+    W = prior if in_place else torch.full_like(prior, 7.0)
+    cq.cqsa_cache_weigh(cache, batch, q, lse, W, prior=prior, decay=0.75)
+    t = torch.arange(n, device="cuda")
+    for b, m in enumerate(lens):
+        k, v = torch.empty(2, 1, max(m, 1), H, d, device="cuda").unbind(0)
+        cq.cqsa_cache_read(cache, cq.CacheBatch(pages[b:b + 1], lengths[b:b + 1]), k, v)
+        del v
+        kk = k[0, max(m, 1) - m:].double().transpose(0, 1).contiguous()
+        qq = q[b].double().view(L, H, G, d).permute(1, 3, 0, 2).reshape(H, d, L * G).contiguous()
+        l = lse[b].double().view(H, G, L).transpose(1, 2).reshape(H, 1, L * G)
+        row = torch.arange(L, device="cuda").repeat_interleave(G)
+        seen = (t[:m, None] <= m - L + row) & (pages[b, t[:m] // page] >= 0)[:, None]
+        w = torch.exp((torch.matmul(kk, qq) * scale - l).masked_fill(~seen, -math.inf)).sum(-1)
+        size = torch.matmul(kk.abs(), qq.abs()) * scale
+        big = torch.maximum(size, l.abs().expand_as(size)).masked_fill(~seen, 0.0).amax(-1)
+        old = max(0, m - L)
+        w[:, :old] += 0.75 * before[b, :, :old]
+        off = (W[b, :, :m].double() - w).abs()
+        assert (off <= w * HALF * ((d + 8) * big + L * G + 16) + 1e-36).all(), (b, off.max().item())
+        behind = before[b, :, m:].float() if in_place else torch.full_like(W[b, :, m:], 7.0)
+        assert torch.equal(W[b, :, m:], behind)
 
 
 def test_strided_tensors_and_another_stream():

@@ -8,6 +8,7 @@ import subprocess
 import pytest
 
 from paper_2604_20819_amd import build
+from tests.op_util import WEIGH_LOOPS
 
 HERE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lanes")
 
@@ -81,3 +82,10 @@ def test_resident_rows_over_many_tiles(weigh, dtype, in_place):
     for d, L, G, lens in ((32, 9, 5, [900, 300]), (96, 33, 1, [600, 33]), (256, 10, 4, [1050])):
         p = weigh(dtype=dtype, d=d, L=L, G=G, lens=lens, tiles=1, in_place=in_place, holes=1, page_log2=5)
         assert p["resident"] and p["a_wave"] >= 3
+
+
+@pytest.mark.parametrize("B,H,G,L,d,dtype,n", WEIGH_LOOPS)
+def test_launches_of_several_tiles(weigh, B, H, G, L, d, dtype, n):
+    """The launches of tests/test_gpu_cache_weigh.py's test of such waves."""
+    p = weigh(lens=[n] * B, H=H, G=G, L=L, d=d, dtype=["f32", "f16", "bf16"].index(dtype), dry=1)
+    assert (p["row_groups"] > 0 or p["resident"]) and p["a_wave"] >= (65 if n > 50000 else 2 if p["resident"] else 3)
