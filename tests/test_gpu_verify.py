@@ -67,6 +67,32 @@ def test_tokens(B, K, V, draft, dtype):
     run(p, q, tokens, u, counts=[int(x) for x in g.integers(-1, K + 2, B)], lengths=[int(x) for x in g.integers(0, 3, B)], alias=True)
 
 
+@pytest.mark.parametrize("B,K,V,dtype,draft", [
+    (130, 1, 70001, "f32", True), (130, 1, 70001, "bf16", False), (129, 2, 100003, "f32", False), (129, 1, 100003, "f16", True),
+    (17, 2, 131073, "f32", True), (18, 1, 200003, "bf16", True), (20, 2, 200003, "f32", False), (19, 2, 262144, "f32", True),
+    (19, 2, 262144, "bf16", False), (3, 1, 1048577, "f16", True), (128, 1, 600001, "bf16", False)])
+def test_large_vocabularies(B, K, V, dtype, draft):
+    """Pieces of the vocabulary that take several loads of a wave, many pieces a wave, and more elements of the drawn
+    piece a thread than it holds: shares of the sum near 0 and 1 too, strange probabilities in some loads of a piece
+    and not in others, refused tokens anywhere."""
+    need_gpu()
+    say("verify large", B, K, V, dtype, draft)
+    p, q, tokens, u = inputs(V + B, B, K, V, dtype, draft, peak=1.0)
+    g = np.random.Generator(np.random.PCG64(B))
+    bad = torch.tensor([math.nan, math.inf, -math.inf, -1.0, -0.0])
+    for b in range(0, B, 3):
+        at = torch.from_numpy(g.integers(0, V, 40))
+        p[b, :, at] = bad[torch.arange(40) % 5].to(p.dtype)
+        if draft:
+            q[b, :, at.roll(1)] = bad[(torch.arange(40) + 2) % 5].to(p.dtype)
+    if not draft:
+        tokens = torch.from_numpy(g.integers(0, V, (B, K), dtype=np.int32))
+    u[1::8, K] = torch.linspace(1e-7, 1e-4, len(u[1::8]))
+    u[2::8, K] = 1 - 2.0 ** -24 * torch.arange(1, len(u[2::8]) + 1)
+    u[::2, 0] = 0.9999
+    run(p, q, tokens, u, counts=[int(x) for x in g.integers(0, K + 1, B)], lengths=[int(x) for x in g.integers(K + 1, 100, B)])
+
+
 def test_draws_over_the_whole_range():
     """One row, many draws: u = 0 is the first token with any probability, near 1 the last."""
     need_gpu()
