@@ -300,6 +300,42 @@ def test_more_sequences_and_heads_than_one_dimension_takes():
     assert torch.equal(W_to, torch.where(gone, 7.0, W.gather(-1, want.clamp(max=31))))
 
 
+def test_work_groups_of_several_chunks():
+    """More long heads than get a work group for each of their chunks of 4096 tokens (2^22 in all): each goes through
+    several.  The same weights for every sequence, of three lengths, as a call of three sequences keeps them."""
+    need_gpu()
+    say("evict many long heads")
+    B, H, T, budget, first, recent = 65536, 2, 140003, 50, 2, 9
+    cache = cq.Cache4(1, H, 32, page_size=256)
+    pages = torch.zeros(B, -(-T // 256), dtype=torch.int32, device="cuda")
+    pages[:, 7] = -1  # the first 256 tokens behind 1792 have no page
+    assert B * H * -(-T // 4096) > 2 ** 22
+    g = torch.Generator("cuda").manual_seed(5)
+    W = torch.rand(1, H, T, generator=g, device="cuda")
+    W = torch.where(W < 0.3, 0.25, W)
+    W[:, 1] = (W[:, 1] * 8).floor()  # many equal ones
+    lens = torch.tensor([T, 33000, 70001], dtype=torch.int32, device="cuda")
+    lengths = lens[torch.arange(B, device="cuda") % 3].contiguous()
+    nowhere = torch.full((B, 1), -1, dtype=torch.int32, device="cuda")
+
+    def run(n, lengths):
+        new = torch.zeros(n, dtype=torch.int32, device="cuda")
+        kept = torch.full((n, H, budget), 7, dtype=torch.int32, device="cuda")
+        W_to = torch.zeros(n, H, budget, device="cuda")
+        cq.cqsa_cache_evict(cache, cq.CacheBatch(pages[:n], lengths, max_len=T), W.expand(n, -1, -1), new, budget, first, recent,
+                            to=nowhere[:n], W_to=W_to, kept=kept)
+        return new, kept, W_to
+
+    few, many = run(3, lens), run(B, lengths)
+    for b, n in enumerate(lens.tolist()):
+        there = np.ones(n, bool)
+        there[7 * 256:8 * 256] = False
+        for h in range(H):
+            assert few[1][b, h].tolist() == ob.keep(W[0, h].cpu().numpy(), there, n, budget, first, recent)
+    for x, y in zip(few, many):
+        assert torch.equal(y, x[torch.arange(B, device="cuda") % 3])
+
+
 def test_weights_far_apart():
     """Weights and pages whose bytes lie past 2^31."""
     need_gpu()
