@@ -175,12 +175,8 @@ cqsa_status attend_impl(const cqsa_cache* c, const cqsa_cache_batch* b, const cq
   a.scale_log2 = (scale > 0.f ? scale : 1.f / std::sqrt(float(c->d))) * kLog2e;
   const AttendPlan p = attend_plan(c, b, *Q);
   const uint64_t need = attend_bytes(p, *Q);
+  if ((st = check_workspace(workspace, workspace_bytes, need, what)) != CQSA_OK) return st;
   if (need > 0) {
-    if (!workspace || workspace_bytes < need)
-      return fail(CQSA_ERR_INVALID_ARG, what + "the workspace has " + std::to_string(workspace ? workspace_bytes : 0) +
-                                            " bytes, the call needs " + std::to_string(need));
-    if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0)
-      return fail(CQSA_ERR_INVALID_ARG, what + "the workspace must be 16-byte aligned");
     const int64_t parts = Q->B * Q->L * Q->H * p.splits;
     a.part = (float*)workspace;
     a.part_ml = a.part + parts * c->d;
