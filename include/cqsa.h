@@ -510,9 +510,9 @@ cqsa_status cqsa_cache_read(const cqsa_cache* cache, const cqsa_cache_batch* bat
 /* Attention of the call's rows Q (H_q heads, a multiple of the cache's H; head h reads the
  * cache's head h / (H_q / H)) over their sequences' cached tokens: with causal = 1 row i of
  * sequence b sees positions 0 ... lengths[b] - n_b + i, with 0 all of them.  O: Q's shape
- * and dtype, Q itself or no element of it (which is checked); LSE (or NULL): fp32 [B, H_q, L], the natural logarithm of the sum of the
- * exponentials of the scaled scores.  A row that sees nothing gets O = 0 and LSE =
- * -infinity.  A NaN in a token reaches only rows that see it.  scale <= 0 selects
+ * and dtype, Q itself or no element of it (which is checked); LSE (or NULL): fp32 [B, H_q, L],
+ * the natural logarithm of the sum of the exponentials of the scaled scores.  A row that sees
+ * nothing gets O = 0 and LSE = -infinity.  A NaN in a token reaches only rows that see it.  scale <= 0 selects
  * 1 / sqrt(d); scale log2(e) must be finite.  Scores and the softmax are fp32 for every dtype.
  * In the product with the values a weight has 16 bits for fp16 and 24 for fp32; for bf16 it has
  * 16, but 8, as in cqsa_forward, where a launch takes 32 rows a work group or more
@@ -560,12 +560,14 @@ typedef struct {
  *   W[b][h][t] = decay prior[b][h][t] + sum over i of exp(s_it - LSE_i),   0 <= t < lengths[b].
  * Q, LSE (fp32 [B, H_q, L]), causal and scale as in cqsa_cache_attend, which leaves that LSE.  prior (or
  * NULL: zeros) is read at the tokens that were there before the call's rows, t < lengths[b] - n_b; the rows'
- * own tokens start from 0 whatever it holds, and with decay = 0 all do.  prior may be W itself, else it lies apart from it; so do
- * the other arguments, Q from its first element to its last (all of which is checked).  W from lengths[b] on is left as it was.  counts: int32 [B] in device memory, or NULL: the sums
- * go over the first counts[b] rows of sequence b alone (taken into [0, n_b]), as where the other rows'
- * drafts were rejected.  Rows whose LSE is not finite (they saw nothing, or a NaN) add nothing; tokens whose
- * page holds nothing get nothing.  decay: in [0, 1].  Scores and sums are fp32 for every dtype; the order of
- * a sum goes by the sizes of the call's arguments alone.
+ * own tokens start from 0 whatever it holds, and with decay = 0 all do.  prior may be W itself, else it lies
+ * apart from it; so do the other arguments, Q from its first element to its last (all of which is checked).
+ * W from lengths[b] on is left as it was.  counts: int32 [B] in device memory, or NULL: the sums go over the
+ * first counts[b] rows of sequence b alone (taken into [0, n_b]), as where the other rows' drafts were
+ * rejected.  Rows whose LSE is not finite (they saw nothing, or a NaN) add nothing; tokens whose page holds
+ * nothing get nothing.  decay: in [0, 1].  Scores and sums are fp32 for every dtype, sums over many rows with
+ * what their additions lose; the order of a sum goes by the sizes of the call's arguments and by the sequence's
+ * own length and rows alone.
  * T of W and prior is at least batch.max_len.  workspace as in cqsa_cache_attend, by
  * cqsa_cache_weigh_workspace.  That call's limits hold, and B H ceil(max_len / 256) is at most 2^27. */
 cqsa_status cqsa_cache_weigh(const cqsa_cache* cache, const cqsa_cache_batch* batch,
@@ -583,21 +585,23 @@ typedef struct {
   int32_t recent; /* and its last ones, >= 0; first + recent <= budget */
 } cqsa_evict_opts;
 
-/* Keep the tokens of most weight.  Every head of a sequence keeps n = min(budget, lengths[b]) tokens: the
- * first ones, the recent ones and of the others those of largest W (of equal ones the earliest; a NaN is below every
- * number).  They stay in their order and become tokens 0 ... n - 1, and new_lengths[b] = n; heads keep
- * different tokens.  Tokens whose page entry holds nothing are never kept and count for no budget (a first or recent
- * one is simply gone).  Keys keep what was written, positions turned into them among it.
+/* Keep the tokens of most weight.  Every head of a sequence keeps n tokens, the smaller of budget and of how
+ * many of its lengths[b] tokens have a page: the first ones, the recent ones and of the others those of largest
+ * W (of equal ones the earliest; a NaN is below every number).  They stay in their order and become tokens
+ * 0 ... n - 1, and new_lengths[b] = n; heads keep different tokens.  Tokens whose page entry holds nothing are
+ * never kept and count for no budget (a first or recent one is simply gone).  Keys keep what was written,
+ * positions turned into them among it.
  * to = NULL: in place; tokens and W move together within the sequence's pages, W_to is NULL, and bytes and
- * weights behind the kept ones stay as they were; a token whose new place's page holds nothing is lost.  Else the kept tokens go to the pages of to's tables
- * (its lengths, q_start and bounds are not read), which share no page with the batch's (what such a page gets is not
- * specified), and the kept tokens' weights to W_to, or nowhere where that is NULL; W stays.  Sequences share pages
- * only where the pages that are written are each one sequence's.
+ * weights behind the kept ones stay as they were; a token whose new place's page holds nothing is lost.  Else
+ * the kept tokens go to the pages of to's tables (its lengths, q_start and bounds are not read), which share no
+ * page with the batch's (what such a page gets is not specified), and the kept tokens' weights to W_to, or
+ * nowhere where that is NULL; W stays.  Sequences share pages only where the pages that are written are each
+ * one sequence's.
  * The batch's q_start and max_q are not read.  W: T at least max_len; W_to: T at least the smaller of budget
  * and max_len, apart from W (checked).  to's tables have pages for that many tokens (checked).
  * kept (or NULL): int32 [B, H, budget], the positions that the kept tokens had, -1 behind them.
- * new_lengths: int32 [B], may be batch.lengths; else what is written lies apart from the other arguments (checked).
- * B H is at most 2^23, and at most 2^27 tiles of 32 tokens may be kept.  workspace as in
+ * new_lengths: int32 [B], may be batch.lengths; else what is written lies apart from the other arguments
+ * (checked).  B H is at most 2^23, and at most 2^27 tiles of 32 tokens may be kept.  workspace as in
  * cqsa_cache_attend, by cqsa_cache_evict_workspace. */
 cqsa_status cqsa_cache_evict(const cqsa_cache* cache, const cqsa_cache_batch* batch,
                              const cqsa_weights* W, const cqsa_evict_opts* opts,

@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(64 * W, W > 8 ? 4 : 2)
   };
 
   // A lane's sums go into a total every 1024 rows, which carries what its own additions lose: added one to
-  // another, weights that are much alike would all round the same way (131072 of them 3.5e-5 off, so 4e-7).
+  // another, weights that are much alike would all round the same way (131072 of them 3.5e-5 off, so 3.7e-7).
   // It lies in LDS, since the registers of 16 waves are all taken (12 would spill at bf16 d = 128).  It takes
   // 0 to 1 % of a call's time, past d = 128 0 to 2 % (one sequence of 4096 tokens and rows of 4 heads, d = 128,
   // 89.5 and 90.1 us; fp32 d = 256 321 and 324).
@@ -502,9 +502,10 @@ constexpr int long_waves(int db) { return db <= 4 ? 16 : 8; }
 // length: not over many sequences, whose lengths differ, and not over few tokens (1 of 8192 tokens and rows,
 // bf16 d = 128 307 us, with 4 waves 333; 4096 rows over 32768 508 and 601; of 3000 72 and 67; 64 of up to 4000,
 // 200 rows, 16 heads a group, 387 and 312; fp16 d = 128, 4 of up to 3000, 198 and 230; d = 160, 64 of 200
-// over 4000, 638 and 599).  4 waves spill at bf16 d = 256 (64 of 200 over 4000 530, with 4 606; of 700 180
-// and 157).  Narrow heads, whose rows take little LDS, have no use for more (bf16 d = 64: 1 of 8192 236, with
-// 4 215; d = 32 206 and 169).
+// over 4000, 638 and 599).  4 waves spill 5 registers at bf16 d = 256 (64 of 200 over 4000 530, with 4 606; of
+// 700 180 and 157), 16 waves spill 4 at fp32 d = 128 (1 of 1024 rows over 16384 294 us, with 4 waves 331; 4096
+// over 8192 522 and 505; 4 of 300 over up to 16384 256 and 272).  Narrow heads, whose rows take little LDS, have
+// no use for more (bf16 d = 64: 1 of 8192 236, with 4 215; d = 32 206 and 169).
 constexpr bool has_long(int parts, int db) { return db > 4 || (db > 1 && parts * db > 2); }
 constexpr bool has_short(int parts, int db) { return db <= 4 || parts < 3; }
 bool takes_long(int parts, int db, int64_t B, int64_t max_len) {

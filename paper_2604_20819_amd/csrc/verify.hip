@@ -87,7 +87,7 @@ __device__ __forceinline__ Rest<T> accept(const VerifyArgs& a, int b, int lane, 
 }
 
 // The largest of the words' elements as unsigned bits: a probability that is negative, NaN or
-// infinite lies at kStrange or above.
+// infinite lies at the bits of infinity or above.
 typedef __attribute__((__vector_size__(4))) unsigned short u16x2;
 template <typename T>
 struct Bits {
